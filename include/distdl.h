@@ -46,7 +46,8 @@ typedef enum {
     DISTDL_ERR_NOMEM = 7
 } distdl_status_t;
 
-typedef enum { DISTDL_F32 = 0, DISTDL_BF16 = 1, DISTDL_F64 = 2 } distdl_dtype_t;
+/* E4M3: one byte, 4 bits of exponent and 3 of mantissa, largest value 448, no infinities; only where a call names it. */
+typedef enum { DISTDL_F32 = 0, DISTDL_BF16 = 1, DISTDL_F64 = 2, DISTDL_E4M3 = 3 } distdl_dtype_t;
 
 #define DISTDL_MAX_RANK 5
 #define DISTDL_MAX_WORKERS 256
@@ -443,6 +444,57 @@ distdl_status_t distdl_affine_adj(int64_t nb, int64_t nfi, int64_t nfo, int32_t 
 distdl_status_t distdl_affine_adj_params(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo,
                                          int32_t pfi, const void *const *dy, const void *const *x,
                                          void *const *dw, void *const *db, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Values in 8 bits with a scale for each block of 128 (an addition of this library; the paper's layers hold fp32).
+ *
+ * A block's scale is s = a / 448 with a = max(2^-100, largest |x| of the block), its values are q = e4m3(x * (448 / a)),
+ * fp32 quotients and products, rounded to nearest even (so |x - q s| is at most 2^-4 |x|, or 2^-10 s for values below 2^-6 s).
+ * The value held is q s.  A block with an infinity or a NaN in it has that scale, and holds NaN or 0 * scale = NaN throughout.
+ *   rows:    blocks of 1 x 128 along the features of one worker's block; the last one of a row may be shorter.
+ *            q[j] E4M3 [nb, nf/pf], s[j] F32 [ceil((nf/pf)/128)][nb]: one scale per row and block, rows contiguous.
+ *   weights: blocks of 128 x 128 of one worker's block; the last ones of a row or column may be smaller.
+ *            q[.] E4M3 [nfo/pfo, nfi/pfi], s[.] F32 [ceil((nfo/pfo)/128)][ceil((nfi/pfi)/128)]; the same values serve
+ *            the layer and its adjoint.
+ * quantize_rows: x[j] [nb, nf/pf] of type t on pf workers; nb = 0 is a no-op.  quantize_weights: w[i*pfi+j]
+ * [nfo/pfo, nfi/pfi] of type t.  t is F32 or BF16.  Any block sizes (nf % pf == 0, nfo % pfo == 0, nfi % pfi == 0, else
+ * DISTDL_ERR_SHAPE); pf <= 8, pfo, pfi <= 8, pfo * pfi <= 16.  Outputs may not overlap inputs.
+ * ---------------------------------------------------------------------- */
+distdl_status_t distdl_quantize_rows(int64_t nb, int64_t nf, int32_t pf, const void *const *x, distdl_dtype_t t,
+                                     void *const *q, void *const *s, void *stream);
+distdl_status_t distdl_quantize_weights(int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *w,
+                                        distdl_dtype_t t, void *const *q, void *const *s, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Root-mean-square norm over features that are split over pf workers, with the addition of the residual in front of it
+ * (the paper's algorithms: every worker's sum of squares, R over the workers, B of the result, a local product -- in one
+ * kernel, the sums and the result stay on the chip).
+ *
+ * rmsnorm_fwd, for every sample b and feature f (feature blocks of nf/pf, the layout that affine_fwd reads):
+ *     h = round_t(x + residual)   (residual == NULL: h = x);   rstd = 1 / sqrt(mean over all nf features of h^2 + eps);
+ *     y = h * rstd * gamma, as y[j] rounded to t and / or as q[j], qs[j] in 8 bits (quantize_rows of the fp32 value).
+ *   x[j], residual[j] [nb, nf/pf] of type t (F32 or BF16); gamma[j] F32 [nf/pf]; eps: HOST pointer to one value > 0.
+ *   Outputs, each list NULL if not wanted: h[j] (may be the residual's or x's own buffers: the sum in place), y[j] of type t,
+ *   q[j] with qs[j]; rstd F32 [nb] or NULL.  y[j] may be x's buffers; no other overlap.  Sums in fp32.
+ * rmsnorm_adj, with h and rstd of the forward pass:
+ *     dh = dres + rstd * (gamma dy - hhat * mean over f of (gamma dy hhat)),  hhat = h * rstd;
+ *     dgamma[f] = sum over b of dy hhat.
+ *   dh is the gradient of x and of the residual alike.  h[j] of type t; dy[j], dres[j] (or dres == NULL) and dh[j]
+ *   [nb, nf/pf] of type tg (F32 or BF16); dh[j] may be dy's or dres's own buffers; gamma[j], dgamma[j] F32 [nf/pf]; dgamma
+ *   may be NULL.  Sums over f and over b in fp32, in an order that depends on the shapes and the device alone: the same
+ *   bits on every run.  workspace: device scratch of at least the size that rmsnorm_adj_workspace reports (at most some
+ *   20 MB), overwritten by the call; calls that may run at the same time need one each.
+ * nf % pf == 0 (else DISTDL_ERR_SHAPE), pf <= 8, any block size up to nf = 2^20; nb = 0: nothing but dgamma = 0.
+ * ---------------------------------------------------------------------- */
+distdl_status_t distdl_rmsnorm_fwd(int64_t nb, int64_t nf, int32_t pf, const void *const *x,
+                                   const void *const *residual, const void *const *gamma, const double *eps,
+                                   distdl_dtype_t t, void *const *h, void *const *y, void *const *q, void *const *qs,
+                                   void *rstd, void *stream);
+distdl_status_t distdl_rmsnorm_adj_workspace(int64_t nb, int64_t nf, int32_t pf, int64_t *bytes);
+distdl_status_t distdl_rmsnorm_adj(int64_t nb, int64_t nf, int32_t pf, const void *const *dy, const void *const *dres,
+                                   const void *const *h, const void *const *gamma, const void *rstd, distdl_dtype_t t,
+                                   distdl_dtype_t tg, void *const *dh, void *const *dgamma, void *workspace,
+                                   int64_t workspace_bytes, void *stream);
 
 /* Synchronises `stream`, then reads and clears the device status word that the affine kernels set
  * when one of their bounded waits (on a shared-memory barrier fed by TMA or by the tensor cores)

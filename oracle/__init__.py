@@ -10,7 +10,9 @@ of the benchmark may call it.  It shares no code, table or helper with the CUDA
 path and imports nothing but numpy.
 
 Every function cites the passage of the paper (Hewett & Grady, "A Linear
-Algebraic Approach to Model Parallelism in Deep Learning") that it restates.
+Algebraic Approach to Model Parallelism in Deep Learning") that it restates;
+the operators of 8-bit affine blocks (module eight_bit), which the paper has not, state
+their definition.
 
 Pin status: every function here is pinned by the CPU tests against something
 other than itself (hand-built operator matrices, values printed in the paper's
@@ -18,6 +20,7 @@ Appendix B figures, closed forms, library routines on the unpartitioned tensor).
 No function is "parity unpinned".
 """
 
+from . import eight_bit  # noqa: F401
 from .partition import Partition, balanced_split, halo_widths_1d  # noqa: F401
 from .primitives import (  # noqa: F401
     broadcast_fwd,

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libdistdl.so")
 F32 = 0
 BF16 = 1
 F64 = 2
+E4M3 = 3
 MAX_RANK = 5
 
 STATUS_NAMES = {
@@ -93,6 +94,11 @@ def lib():
     L.distdl_convg_adj.argtypes = [vp, c_i64, c_i32, pvp, pvp, c_i32, c_i32, pvp, vp]
     L.distdl_convg_adj_params_workspace.argtypes = [vp, c_i64, c_i32, c_i32, c_i32, pi64]
     L.distdl_convg_adj_params.argtypes = [vp, c_i64, c_i32, pvp, pvp, c_i32, c_i32, pvp, pvp, vp, c_i64, vp]
+    L.distdl_quantize_rows.argtypes = [c_i64, c_i64, c_i32, pvp, c_i32, pvp, pvp, vp]
+    L.distdl_quantize_weights.argtypes = [c_i64, c_i64, c_i32, c_i32, pvp, c_i32, pvp, pvp, vp]
+    L.distdl_rmsnorm_fwd.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, vp, c_i32, pvp, pvp, pvp, pvp, vp, vp]
+    L.distdl_rmsnorm_adj_workspace.argtypes = [c_i64, c_i64, c_i32, pi64]
+    L.distdl_rmsnorm_adj.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, pvp, vp, c_i32, c_i32, pvp, pvp, vp, c_i64, vp]
     L.distdl_device_status.argtypes = [vp]
     L.distdl_selftest_wait_timeout.argtypes = [c_i64, vp]
     L.distdl_selftest_row_plan.argtypes = [vp, c_i32, pi32, c_i32, pi32, c_i32, pi32]
@@ -515,6 +521,111 @@ def conv_adj_params(part, x, dy, kernel, dw, db, workspace, stream=None):
     n = part.num_workers
     _check((_calls or _load()).conv_adj_params(part._address, x, dy, kernel[0], kernel[1], dw, db, workspace,
                                                workspace.numel() * workspace.element_size(), stream, n, n))
+
+
+_types = {}
+
+
+def _float_code(what, ts):
+    """(code, dtype) of the values of a list: F32 or BF16, by its first tensor."""
+    if not _types:
+        import torch
+        _types.update({torch.float32: F32, torch.bfloat16: BF16})
+        _types["e4m3"], _types["f32"], _types["bf16"] = torch.float8_e4m3fn, torch.float32, torch.bfloat16
+    if not len(ts):
+        raise DistdlError(1, "%s is an empty list" % what)
+    dtype = ts[0].dtype
+    code = _types.get(dtype)
+    if code is None:
+        raise TypeError("%s: values of type %s" % (what, dtype))
+    return code, dtype
+
+
+def _need(what, ts, n, numel, dtype):
+    """Refuses a list of blocks that is too short, and blocks of another type, size or layout than the kernels take them for (a raw
+    address says neither; the library has the last word on it)."""
+    if ts is None:
+        return
+    if len(ts) < n:
+        raise DistdlError(1, "%s is a list of %d entries, %d are needed" % (what, len(ts), n))
+    for t in ts:
+        if t.__class__ is not int and (t.dtype is not dtype or t.numel() != numel or not t.is_contiguous()):
+            raise DistdlError(2, "%s: contiguous blocks of %d elements of type %s are needed" % (what, numel, dtype))
+
+
+def _features(what, n, workers):
+    if workers < 1 or n % workers:
+        raise DistdlError(2, "%s: %d features on %d workers" % (what, n, workers))
+    return n // workers
+
+
+def _blocks128(n):
+    return -(-n // 128)
+
+
+def quantize_rows(nb, nf, pf, x, q, s, stream=None):
+    """Values of x[j] [nb, nf/pf] in 8 bits, q[j] float8_e4m3fn, and a scale for every 128 features of a row, s[j] float32
+    [ceil((nf/pf)/128), nb]."""
+    code, dtype = _float_code("x", x)
+    bf = _features("quantize_rows", nf, pf)
+    _need("x", x, pf, nb * bf, dtype)
+    _need("q", q, pf, nb * bf, _types["e4m3"])
+    _need("s", s, pf, nb * _blocks128(bf), _types["f32"])
+    _check((_calls or _load()).quantize_rows(nb, nf, pf, x, code, q, s, stream, pf, pf, pf))
+
+
+def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
+    """Blocks of weights w[i * pfi + j] [nfo/pfo, nfi/pfi] in 8 bits, q float8_e4m3fn, and a scale for every 128 x 128, s float32
+    [ceil((nfo/pfo)/128), ceil((nfi/pfi)/128)]."""
+    code, dtype = _float_code("w", w)
+    bfi, bfo, n = _features("quantize_weights", nfi, pfi), _features("quantize_weights", nfo, pfo), pfo * pfi
+    _need("w", w, n, bfo * bfi, dtype)
+    _need("q", q, n, bfo * bfi, _types["e4m3"])
+    _need("s", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"])
+    _check((_calls or _load()).quantize_weights(nfi, nfo, pfo, pfi, w, code, q, s, stream, n, n, n))
+
+
+def rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, h=None, y=None, q=None, qs=None, rstd=None, stream=None):
+    """h = x + residual (residual None: x), rstd = 1 / sqrt(mean h^2 + eps), h * rstd * gamma as y (type of x) and / or as q, qs in 8
+    bits; each output may be None.  Lists of feature blocks [nb, nf/pf]; h may be the residual's own blocks."""
+    code, dtype = _float_code("x", x)
+    bf = _features("rmsnorm_fwd", nf, pf)
+    f32 = _types["f32"]
+    _need("x", x, pf, nb * bf, dtype)
+    _need("residual", residual, pf, nb * bf, dtype)
+    _need("gamma", gamma, pf, bf, f32)
+    _need("h", h, pf, nb * bf, dtype)
+    _need("y", y, pf, nb * bf, dtype)
+    _need("q", q, pf, nb * bf, _types["e4m3"])
+    _need("qs", qs, pf, nb * _blocks128(bf), f32)
+    if rstd is not None:
+        _need("rstd", (rstd,), 1, nb, f32)
+    _check((_calls or _load()).rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, code, h, y, q, qs, rstd, stream, pf, pf, pf, pf, pf, pf, pf))
+
+
+def rmsnorm_adj_workspace(nb, nf, pf):
+    """Bytes of device scratch rmsnorm_adj needs on the current device."""
+    n = ctypes.c_int64(0)
+    _check(lib().distdl_rmsnorm_adj_workspace(nb, nf, pf, ctypes.byref(n)))
+    return n.value
+
+
+def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, stream=None):
+    """Gradient dh of x and of the residual (dres: the gradient that reaches their sum past the norm, or None), and dgamma (or None);
+    h and rstd as rmsnorm_fwd left them; workspace: a uint8 tensor."""
+    code, dtype = _float_code("h", h)
+    gcode, gdtype = _float_code("dy", dy)
+    bf = _features("rmsnorm_adj", nf, pf)
+    f32 = _types["f32"]
+    _need("dy", dy, pf, nb * bf, gdtype)
+    _need("dres", dres, pf, nb * bf, gdtype)
+    _need("h", h, pf, nb * bf, dtype)
+    _need("gamma", gamma, pf, bf, f32)
+    _need("rstd", (rstd,), 1, nb, f32)
+    _need("dh", dh, pf, nb * bf, gdtype)
+    _need("dgamma", dgamma, pf, bf, f32)
+    _check((_calls or _load()).rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
+                                           workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
 
 
 def device_status(stream=None):

@@ -76,13 +76,51 @@ struct Arg<const float *> {                           // what taps() returns
     const float *get() { return value; }
 };
 
-struct Pointers {                                     // shards; None: no array
+template <>
+struct Arg<const double *> {                          // a number, or up to eight of them
+    double value[8] = {};
+    bool read(PyObject *o, bool) {
+        if (PyNumber_Check(o)) {
+            value[0] = PyFloat_AsDouble(o);
+            return !PyErr_Occurred();
+        }
+        PyObject *s = PySequence_Tuple(o);
+        if (!s) return false;
+        const Py_ssize_t n = PyTuple_GET_SIZE(s);
+        bool ok = n <= 8;
+        if (!ok) PyErr_SetString(PyExc_ValueError, "at most eight numbers");
+        for (Py_ssize_t i = 0; ok && i < n; ++i) {
+            value[i] = PyFloat_AsDouble(PyTuple_GET_ITEM(s, i));
+            ok = !PyErr_Occurred();
+        }
+        Py_DECREF(s);
+        return ok;
+    }
+    const double *get() { return value; }
+};
+
+template <>
+struct Arg<const int64_t *> {                         // packed in bytes
+    const int64_t *value;
+    bool read(PyObject *o, bool) {
+        value = reinterpret_cast<const int64_t *>(PyBytes_AsString(o));
+        return value != nullptr;
+    }
+    const int64_t *get() { return value; }
+};
+
+struct Pointers {                                     // shards, or their addresses packed in bytes; None: no array
     void *few[64] = {};
     std::vector<void *> many;
     void **p = nullptr;
     Py_ssize_t size = 0;
     bool read(PyObject *o, bool) {
         if (o == Py_None) return true;
+        if (PyBytes_Check(o)) {
+            p = reinterpret_cast<void **>(PyBytes_AS_STRING(o));
+            size = PyBytes_GET_SIZE(o) / (Py_ssize_t)sizeof(void *);
+            return true;
+        }
         PyObject *s = PySequence_Fast(o, "a sequence of shards is needed");
         if (!s) return false;
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(s);
@@ -196,6 +234,7 @@ PyMethodDef methods[] = {
     FUNCTION(conv_fwd), FUNCTION(conv_adj), FUNCTION(conv_adj_params), FUNCTION(convg_fwd), FUNCTION(convg_adj), FUNCTION(convg_adj_params),
     FUNCTION(stencil3d_fwd), FUNCTION(stencil3d_adj), FUNCTION(pool_fwd), FUNCTION(pool_adj),
     FUNCTION(affine_fwd), FUNCTION(affine_adj), FUNCTION(affine_adj_params),
+    FUNCTION(quantize_rows), FUNCTION(quantize_weights), FUNCTION(rmsnorm_fwd), FUNCTION(rmsnorm_adj),
     {"taps", taps, METH_O, nullptr},
     {"set_stream_lookup", (PyCFunction)(void (*)(void))set_stream_lookup, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -1,0 +1,271 @@
+"""GPU tests of the operators of 8-bit affine blocks against the oracle (fp64), at the sizes and values where they can go wrong.
+
+Tolerances count the roundings: half a step of the type for a value that is rounded to it (bfloat16 2^-8, fp32 2^-24 relative), n 2^-24
+of the sum of magnitudes for an fp32 sum with n additions on a path.
+"""
+
+import numpy as np
+import pytest
+
+import paper_2006_03108_b200 as distdl
+from oracle import eight_bit as o
+from paper_2006_03108_b200 import inputs
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+E4 = torch.float8_e4m3fn
+U = 2.0 ** -24
+GUARD = 64                                      # elements on either side of an output that have to stay
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.array(a)).to(DEV).to(dtype)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+class Out:
+    """Outputs in buffers of garbage; `check` looks at what lies around them."""
+
+    def __init__(self):
+        self.held = []
+
+    def __call__(self, *shape, dtype=torch.float32):
+        n = int(np.prod(shape))
+        buf = torch.full(((n + 2 * GUARD) * dtype.itemsize,), 0x5b, dtype=torch.uint8, device=DEV).view(dtype)
+        self.held.append((buf, n))
+        return buf[GUARD:GUARD + n].view(*shape)
+
+    def check(self):
+        for buf, n in self.held:
+            b = buf.view(torch.uint8)
+            size = buf.dtype.itemsize
+            assert (b[:GUARD * size] == 0x5b).all() and (b[(GUARD + n) * size:] == 0x5b).all()
+
+
+def rounded(a, t):
+    """fp32 numbers as a tensor of a type holds them."""
+    return a.astype(np.float32) if t is torch.float32 else inputs.bf16_bits_to_f32(inputs.f32_to_bf16_bits(a))
+
+
+def eps_of(t):
+    return 2.0 ** -8 if t is torch.bfloat16 else 2.0 ** -24
+
+
+def same_quant(q, s, want):
+    assert np.array_equal(f64(q), want[0], equal_nan=True) and np.array_equal(s.cpu().numpy(), want[1], equal_nan=True)
+
+
+BF = [1, 7, 8, 16, 100, 127, 128, 129, 130, 250, 1250, 2048, 2052]
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bf", BF)
+@pytest.mark.parametrize("nb,pf", [(1, 1), (3, 2), (17, 3), (40, 8)])
+def test_quantize_rows_to_the_bit(t, bf, nb, pf):
+    x = [rounded(inputs.normal((nb, bf), 10 + j) * np.float32(10.0) ** inputs.integers((nb, 1), 90 + j, -6, 7), t) for j in range(pf)]
+    out = Out()
+    q, s = [out(nb, bf, dtype=E4) for _ in range(pf)], [out(-(-bf // 128), nb) for _ in range(pf)]
+    distdl.quantize_rows(nb, bf * pf, pf, [dev(a, t) for a in x], q, s)
+    for a, b, c in zip(x, q, s):
+        same_quant(b, c, o.quantize_rows(a))
+    out.check()
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bfo,bfi,pfo,pfi", [(1, 1, 1, 1), (128, 128, 1, 1), (129, 127, 2, 1), (250, 130, 1, 3), (64, 516, 2, 2), (300, 1000, 1, 2), (7, 2050, 4, 4)])
+def test_quantize_weights_to_the_bit(t, bfo, bfi, pfo, pfi):
+    w = [rounded(inputs.normal((bfo, bfi), 20 + i, 0.02 * (i + 1)), t) for i in range(pfo * pfi)]
+    out = Out()
+    q, s = [out(bfo, bfi, dtype=E4) for _ in w], [out(-(-bfo // 128), -(-bfi // 128)) for _ in w]
+    distdl.quantize_weights(bfi * pfi, bfo * pfo, pfo, pfi, [dev(a, t) for a in w], q, s)
+    for a, b, c in zip(w, q, s):
+        same_quant(b, c, o.quantize_weights(a))
+    out.check()
+
+
+@pytest.mark.parametrize("weights", [False, True], ids=["rows", "weights"])
+def test_quantize_special_values(weights):
+    """Zeros, the smallest and largest numbers, infinities and NaN: a block's fate is its own."""
+    x = inputs.normal((8, 640), 5)
+    x[0, :128] = 0.0
+    x[1] = 0.0
+    x[2, 128:256] = 1e-45                       # below every normal number
+    x[3, 256:384] *= np.float32(3e38 / 5)
+    x[4, 130] = np.inf
+    x[5, 300] = np.nan
+    x[6, 5] = -np.inf
+    x[7, 639] = -0.0
+    a = np.ascontiguousarray(x.repeat(128, 0)) if weights else x
+    q, s = torch.empty(*a.shape, dtype=E4, device=DEV), torch.empty((8, 5) if weights else (5, 8), device=DEV)
+    if weights:
+        distdl.quantize_weights(640, 1024, 1, 1, [dev(a)], [q], [s])
+    else:
+        distdl.quantize_rows(8, 640, 1, [dev(a)], [q], [s])
+    with np.errstate(invalid="ignore", over="ignore"):
+        value = f64(q) * np.repeat(np.repeat(f64(s), 128, 0), 128, 1) if weights else o.row_values(f64(q), s.cpu().numpy())
+        value = value[::128] if weights else value
+    bad = np.zeros((8, 5), bool)
+    bad[4, 1] = bad[5, 2] = bad[6, 0] = True
+    bad = np.repeat(bad, 128, 1)
+    assert np.isnan(value[bad]).all() and np.isfinite(value[~bad]).all()
+    want = o.quantize_rows(np.where(bad, 0, x))
+    ok = np.repeat(want[1].T, 128, 1)
+    assert np.array_equal(value[~bad], (want[0] * ok)[~bad]) and (value[1] == 0).all() and (value[2, 128:256] == 0).all()
+
+
+NORM = [(1, 1, 1), (3, 1, 2), (2, 8192, 1), (5, 100, 8), (300, 128, 1), (297, 40, 3), (400, 1250, 4), (9, 5000, 2), (310, 2048, 4), (2, 16384, 2), (3, 5003, 8), (700, 8, 1),
+        (301, 16500, 2)]
+
+
+def norm_inputs(nb, bf, pf, t, seed=40):
+    x = [rounded(inputs.normal((nb, bf), seed + j, 2.0), t) for j in range(pf)]
+    r = [rounded(inputs.normal((nb, bf), seed + 20 + j), t) for j in range(pf)]
+    g = [1 + inputs.normal((bf,), seed + 40 + j, 0.2) for j in range(pf)]
+    return x, r, g
+
+
+def sum_error(n_features, pf):
+    """Additions on a path of the kernel's sum over a sample's features: at most eight for each chunk of a thread, ten through its
+    group; the chunks (padded to blocks of 128 per worker) are spread over a thread for every four or more, up to 1024 of them."""
+    chunks = pf * -(-(n_features // pf) // 128) * 16
+    return (8 * max(4, -(-chunks // 512)) + 12) * U
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("nb,bf,pf", NORM)
+def test_rmsnorm_fwd(t, nb, bf, pf):
+    eps, nf = 1e-5, bf * pf
+    x, r, g = norm_inputs(nb, bf, pf, t)
+    out = Out()
+    h, y = [out(nb, bf, dtype=t) for _ in range(pf)], [out(nb, bf, dtype=t) for _ in range(pf)]
+    q, qs = [out(nb, bf, dtype=E4) for _ in range(pf)], [out(-(-bf // 128), nb) for _ in range(pf)]
+    rstd = out(nb)
+    distdl.rmsnorm_fwd(nb, nf, pf, [dev(a, t) for a in x], [dev(a, t) for a in r], [dev(a) for a in g], eps, h, y, q, qs, rstd)
+    hw = [rounded(a + b, t).astype(np.float64) for a, b in zip(x, r)]          # fp32 sum, rounded to the type
+    for a, b in zip(h, hw):
+        assert np.array_equal(f64(a), b)
+    yw, rw = o.rmsnorm_fwd(hw, [a.astype(np.float64) for a in g], float(np.float32(eps)))
+    re = sum_error(nf, pf) / 2 + 4 * U                                          # half of the sum's; mean, + eps, root, quotient
+    assert (np.abs(f64(rstd) - rw) <= re * rw).all()
+    for j in range(pf):
+        ye = (re + 3 * U) * np.abs(yw[j])
+        assert (np.abs(f64(y[j]) - yw[j]) <= ye + eps_of(t) * (np.abs(yw[j]) + ye)).all()
+        v, scale = o.row_values(f64(q[j]), qs[j].cpu().numpy()), np.repeat(f64(qs[j]).T, 128, 1)[:, :bf]
+        assert (np.abs(v - yw[j]) <= np.maximum(2.0 ** -4 * np.abs(yw[j]), 2.0 ** -10 * scale) * (1 + 4 * U) + 2 * ye).all()
+        if t is torch.float32:                                                  # y is the value that is quantised
+            same_quant(q[j], qs[j], o.quantize_rows(y[j].cpu().numpy()))
+    out.check()
+    # without a residual, one output at a time, and the sum in place of the residual: the same values
+    hx = [dev(a, t) for a in hw]
+    for keep in ("y", "q", "rstd"):
+        y2, q2, s2, r2 = [torch.zeros_like(a) for a in y], [torch.zeros_like(a) for a in q], [torch.zeros_like(a) for a in qs], torch.zeros_like(rstd)
+        distdl.rmsnorm_fwd(nb, nf, pf, hx, None, [dev(a) for a in g], eps, None, y2 if keep == "y" else None, q2 if keep == "q" else None,
+                           s2 if keep == "q" else None, r2 if keep == "rstd" else None)
+        for a, b in {"y": zip(y, y2), "q": list(zip(q, q2)) + list(zip(qs, s2)), "rstd": [(rstd, r2)]}[keep]:
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    rd = [dev(a, t) for a in r]
+    distdl.rmsnorm_fwd(nb, nf, pf, [dev(a, t) for a in x], rd, [dev(a) for a in g], eps, rd)
+    for a, b in zip(rd, h):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("tg", [torch.float32, torch.bfloat16], ids=["gf32", "gbf16"])
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("nb,bf,pf", NORM)
+@pytest.mark.parametrize("res", [True, False], ids=["res", "nores"])
+def test_rmsnorm_adj(t, tg, nb, bf, pf, res):
+    nf = bf * pf
+    h, _, g = norm_inputs(nb, bf, pf, t, 140)
+    dy = [rounded(inputs.normal((nb, bf), 200 + j, 0.1), tg) for j in range(pf)]
+    dres = [rounded(inputs.normal((nb, bf), 220 + j, 0.1), tg) for j in range(pf)] if res else None
+    rstd = (1 / np.sqrt(sum((a.astype(np.float64) ** 2).sum(1) for a in h) / nf + 1e-5)).astype(np.float32)
+    out = Out()
+    dh, dg = [out(nb, bf, dtype=tg) for _ in range(pf)], [out(bf) for _ in range(pf)]
+    ws = out(distdl.rmsnorm_adj_workspace(nb, nf, pf), dtype=torch.uint8)
+    args = [dev(a, t) for a in h], [dev(a) for a in g], dev(rstd)
+    dy_d, dres_d = [dev(a, tg) for a in dy], [dev(a, tg) for a in dres] if res else None
+    distdl.rmsnorm_adj(nb, nf, pf, dy_d, dres_d, *args, dh, dg, ws)
+    h64, g64, d64 = ([a.astype(np.float64) for a in v] for v in (h, g, dy))
+    dhw, dgw = o.rmsnorm_adj(d64, [a.astype(np.float64) for a in dres] if res else None, h64, g64, rstd)
+    r = rstd.astype(np.float64)[:, None]
+    terms = sum((np.abs(a * b * c)).sum(1, keepdims=True) for a, b, c in zip(d64, h64, g64)) / nf
+    total = nb if nb < 20 else 20 + nb / 8                # additions on a path of dgamma: samples of a block, groups, blocks
+    for j in range(pf):
+        back = np.abs(h64[j]) * r ** 3 * terms
+        e = (sum_error(nf, pf) + 8 * U) * back + 4 * U * (np.abs(r * g64[j] * d64[j]) + (np.abs(dres[j]) if res else 0) + back)
+        assert (np.abs(f64(dh[j]) - dhw[j]) <= e + eps_of(tg) * (np.abs(dhw[j]) + e)).all()
+        assert (np.abs(f64(dg[j]) - dgw[j]) <= (total + 4) * U * np.abs(d64[j] * h64[j] * r).sum(0)).all()
+    out.check()
+    # the same bits again; without dgamma; in place of dy and of dres
+    again = [torch.empty_like(a) for a in dg]
+    distdl.rmsnorm_adj(nb, nf, pf, dy_d, dres_d, *args, dy_d, again, ws)
+    assert all(torch.equal(a, b) for a, b in zip(again, dg)) and all(torch.equal(a, b) for a, b in zip(dy_d, dh))
+    if res:
+        distdl.rmsnorm_adj(nb, nf, pf, [dev(a, tg) for a in dy], dres_d, *args, dres_d, None, ws)
+        assert all(torch.equal(a, b) for a, b in zip(dres_d, dh))
+
+
+def test_rmsnorm_gradient_against_differences():
+    """<dh, way> and <dgamma, way> against central differences of the fp64 definition."""
+    nb, bf, pf, eps = 5, 333, 3, 1e-5
+    h, way, g = norm_inputs(nb, bf, pf, torch.float32, 300)
+    h64, w64, g64 = ([a.astype(np.float64) for a in v] for v in (h, way, g))
+    dy = [inputs.normal((nb, bf), 360 + j) for j in range(pf)]
+    rstd = torch.empty(nb, device=DEV)
+    hd, gd = [dev(a) for a in h], [dev(a) for a in g]
+    distdl.rmsnorm_fwd(nb, bf * pf, pf, hd, None, gd, eps, rstd=rstd)
+    dh, dg = [torch.empty_like(a) for a in hd], [torch.empty_like(a) for a in gd]
+    distdl.rmsnorm_adj(nb, bf * pf, pf, [dev(a) for a in dy], None, hd, gd, rstd, dh, dg,
+                       torch.empty(distdl.rmsnorm_adj_workspace(nb, bf * pf, pf), dtype=torch.uint8, device=DEV))
+    loss = lambda a, b: sum((u * v).sum() for u, v in zip(o.rmsnorm_fwd([x + a * w for x, w in zip(h64, w64)], [x + b * w[0] for x, w in zip(g64, w64)], eps)[0], dy))  # noqa: E731
+    step = 1e-5
+    for got, want, scale in ((sum((f64(a) * b).sum() for a, b in zip(dh, w64)), (loss(step, 0) - loss(-step, 0)) / (2 * step), sum(np.abs(f64(a) * b).sum() for a, b in zip(dh, w64))),
+                             (sum((f64(a) * b[0]).sum() for a, b in zip(dg, w64)), (loss(0, step) - loss(0, -step)) / (2 * step), sum(np.abs(f64(a) * b[0]).sum() for a, b in zip(dg, w64)))):
+        assert abs(got - want) <= 1e-6 * scale
+
+
+def test_rmsnorm_of_a_bad_sample_is_its_own():
+    """Infinity or NaN in a sample stays in that sample (dgamma sums over all of them)."""
+    nb, bf, pf = 40, 136, 2
+    x, _, g = norm_inputs(nb, bf, pf, torch.float32, 400)
+    clean = [a.copy() for a in x]
+    x[0][7, 3], x[1][20, 135], x[0][39, 0] = np.inf, np.nan, -np.inf
+    for a in clean:
+        a[[7, 20, 39]] = 0.0
+    bad = np.isin(np.arange(nb), [7, 20, 39])
+    res = []
+    for v in (x, clean):
+        xd, gd = [dev(a) for a in v], [dev(a) for a in g]
+        y, q, s = [torch.empty_like(a) for a in xd], [torch.empty(nb, bf, dtype=E4, device=DEV) for _ in xd], [torch.empty(2, nb, device=DEV) for _ in xd]
+        rstd, dh = torch.empty(nb, device=DEV), [torch.empty_like(a) for a in xd]
+        distdl.rmsnorm_fwd(nb, bf * pf, pf, xd, None, gd, 1e-6, None, y, q, s, rstd)
+        ws = torch.empty(distdl.rmsnorm_adj_workspace(nb, bf * pf, pf), dtype=torch.uint8, device=DEV)
+        distdl.rmsnorm_adj(nb, bf * pf, pf, y, None, xd, gd, rstd, dh, None, ws)
+        res.append([f64(a)[~bad] for a in y + q + dh] + [f64(a)[:, ~bad] for a in s] + [f64(rstd)[~bad]])
+        if v is x:
+            assert np.isnan(f64(y[0])[20]).all() and np.isnan(f64(y[0])[7, 3])
+    assert all(np.array_equal(a, b) and np.isfinite(a).all() for a, b in zip(*res))
+    # a sample of zeros is normed to zeros
+    assert (f64(rstd)[7] == np.float32(1) / np.sqrt(np.float32(1e-6))).all() and (f64(y[0])[7] == 0).all() and (f64(q[1])[7] == 0).all()
+
+
+def test_rmsnorm_of_no_samples():
+    dg = [torch.full((130,), 5.0, device=DEV) for _ in range(2)]
+    e = [torch.empty(0, 130, device=DEV) for _ in range(2)]
+    distdl.rmsnorm_fwd(0, 260, 2, e, e, dg, 1e-6, e, e)
+    assert all((a == 5).all() for a in dg)
+    distdl.rmsnorm_adj(0, 260, 2, e, None, e, dg, e[0].view(0), e, dg, torch.empty(16, dtype=torch.uint8, device=DEV))
+    assert all((a == 0).all() for a in dg)
+    distdl.quantize_rows(0, 260, 2, e, [a.to(E4) for a in e], [torch.empty(2, 0, device=DEV)] * 2)
+    torch.cuda.synchronize()
+
+
+def test_host_memory_is_refused():
+    t = torch.zeros(4, 128)
+    with pytest.raises(distdl.DistdlError) as e:
+        distdl.quantize_rows(4, 128, 1, [t], [t.to(E4)], [torch.zeros(1, 4)])
+    assert e.value.status == 1
