@@ -496,6 +496,34 @@ distdl_status_t distdl_rmsnorm_adj(int64_t nb, int64_t nf, int32_t pf, const voi
                                    distdl_dtype_t tg, void *const *dh, void *const *dgamma, void *workspace,
                                    int64_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * AdamW over `count` tensors at once: the step from the gradients of the *_adj_params calls to new weights (an addition of
+ * this library).  For every element, with the gradient g scaled by c:
+ *     m = beta1 m + (1 - beta1) c g;   v = beta2 v + (1 - beta2) (c g)^2;
+ *     p = p - lr * decay * p - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)     (decoupled weight decay)
+ * p[i], m[i], v[i] are updated in place; elems[i] >= 0 elements each (0: nothing, its buffers may be NULL).  p[i] F32;
+ * g[i] of type tg (F32 or BF16), read only; copies[i] BF16 (or NULL, or copies == NULL): receives the new p, rounded to
+ * nearest even, for the layers that take bfloat16 weights.
+ * state F32: m[i], v[i] F32; ms, vs are not looked at.
+ * state E4M3: the moments are held in 8 bits with a scale for every 128 elements, ms[i], vs[i] F32 [ceil(elems[i]/128)]:
+ *     m = code * scale;  v = (code * scale)^2, the root of the second moment is what is held.  Scales as in quantize_rows;
+ *     codes are rounded up or down at random so that their mean is the value (to the nearest, a decay of 0.1 % a step would
+ *     never leave a code): floor(x / d + u) * d, d the distance of the codes at x, u of 16 random bits of (seed, t, tensor,
+ *     element); a second moment that is not zero is held as no less than the smallest code.  All zero bits are a fresh state.
+ *     The step itself uses the moments before they are rounded.
+ * hyper: HOST array {lr, beta1, beta2, eps, decay, c};  step: t >= 1, the same for all tensors.
+ * live: NULL, or a DEVICE array F32 {lr, t, c} that is read when the step runs and stands in the place of those three, for
+ *     steps that are captured in a graph and replayed (t is exact up to 2^24).
+ * count <= DISTDL_MAX_TENSORS.  One launch for every 320 tensors.  Buffers that are written may not overlap any other
+ * buffer of the call (not detected: undefined results).  Every element's result depends on that element, and in 8 bits on
+ * its block of 128, alone; fp32 throughout.
+ * ---------------------------------------------------------------------- */
+#define DISTDL_MAX_TENSORS 4096
+distdl_status_t distdl_adamw_step(int32_t count, const int64_t *elems, void *const *p, const void *const *g,
+                                  distdl_dtype_t tg, void *const *m, void *const *v, void *const *ms, void *const *vs,
+                                  distdl_dtype_t state, void *const *copies, const double *hyper, int64_t step,
+                                  int64_t seed, const void *live, void *stream);
+
 /* Synchronises `stream`, then reads and clears the device status word that the affine kernels set
  * when one of their bounded waits (on a shared-memory barrier fed by TMA or by the tensor cores)
  * ran out: DISTDL_ERR_TIMEOUT in that case (the outputs of that launch are then undefined),

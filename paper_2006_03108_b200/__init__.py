@@ -13,6 +13,7 @@ import ctypes
 import importlib
 import math
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdistdl.so")
@@ -99,6 +100,7 @@ def lib():
     L.distdl_rmsnorm_fwd.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, vp, c_i32, pvp, pvp, pvp, pvp, vp, vp]
     L.distdl_rmsnorm_adj_workspace.argtypes = [c_i64, c_i64, c_i32, pi64]
     L.distdl_rmsnorm_adj.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, pvp, vp, c_i32, c_i32, pvp, pvp, vp, c_i64, vp]
+    L.distdl_adamw_step.argtypes = [c_i32, pi64, pvp, pvp, c_i32, pvp, pvp, pvp, pvp, c_i32, pvp, vp, c_i64, c_i64, vp, vp]
     L.distdl_device_status.argtypes = [vp]
     L.distdl_selftest_wait_timeout.argtypes = [c_i64, vp]
     L.distdl_selftest_row_plan.argtypes = [vp, c_i32, pi32, c_i32, pi32, c_i32, pi32]
@@ -626,6 +628,70 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
     _need("dgamma", dgamma, pf, bf, f32)
     _check((_calls or _load()).rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
                                            workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
+
+
+class AdamW:
+    """Weights p (float32 tensors) and the state of their optimiser, the step of all of them in one call (distdl_adamw_step in
+    include/distdl.h).
+
+    m, v: float32, or float8_e4m3fn with scales ms, vs (float32, one for every 128 elements); zeros are a fresh state.  copies:
+    bfloat16 tensors that receive the new weights, or None for some or all.  The tensors are checked and their addresses taken here:
+    they have to stay where they are (in-place operations and loads are fine) as long as the handle is used."""
+
+    def __init__(self, p, m, v, ms=None, vs=None, copies=None):
+        import torch
+        _load()
+        n = len(p)
+        if n and m and len(m) and m[0].dtype is torch.float8_e4m3fn:
+            self._state, held = E4M3, torch.float8_e4m3fn
+            if ms is None or vs is None:
+                raise DistdlError(1, "AdamW: states in 8 bits need their scales")
+        else:
+            self._state, held, ms, vs = F32, torch.float32, None, None
+        written, self._elems = [], [t.numel() for t in p]
+        self._device = p[0].device if n else None
+        lists = (("p", p, torch.float32), ("m", m, held), ("v", v, held), ("ms", ms, torch.float32), ("vs", vs, torch.float32),
+                 ("copies", copies, torch.bfloat16))
+        for name, ts, dtype in lists:
+            if ts is None:
+                continue
+            if len(ts) != n:
+                raise DistdlError(1, "AdamW: %s is a list of %d entries, %d are needed" % (name, len(ts), n))
+            for t, k in zip(ts, self._elems):
+                if t is None and name == "copies":
+                    continue
+                size = _blocks128(k) if name in ("ms", "vs") else k
+                if t.dtype is not dtype or t.numel() != size or not t.is_contiguous() or t.device != self._device:
+                    raise DistdlError(2, "AdamW: %s: contiguous tensors of the weights' sizes and device, type %s, are needed" % (name, dtype))
+                if size:
+                    written.append((t.data_ptr(), t.data_ptr() + size * t.element_size()))
+        written.sort()
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise DistdlError(1, "AdamW: tensors overlap")
+        self._keep = [ts for _, ts, _ in lists]
+        self._count, self._bytes = n, struct.pack("%dq" % n, *self._elems)
+        self._p, self._m, self._v, self._ms, self._vs, self._copies = [
+            None if ts is None else struct.pack("%dQ" % n, *[0 if t is None else t.data_ptr() for t in ts]) for ts in self._keep]
+
+    def step(self, g, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, seed=0, grad_scale=1.0, live=None, stream=None):
+        """One step (the step-th, from 1) with gradients g (float32 or bfloat16); seed: of the rounding of states in 8 bits; live: a
+        float32 device tensor [lr, step, grad_scale] read when the step runs, in the place of these three."""
+        n = self._count
+        if not n:
+            return
+        if len(g) != n:
+            raise DistdlError(1, "AdamW: g is a list of %d entries, %d are needed" % (len(g), n))
+        code, dtype = _float_code("g", g)
+        device = self._device
+        for t, k in zip(g, self._elems):
+            if t.dtype is not dtype or t.numel() != k or not t.is_contiguous() or t.device != device:
+                raise DistdlError(2, "AdamW: g: contiguous tensors of the weights' sizes and device, of one type, are needed")
+        if live is not None:
+            _need("live", (live,), 1, 3, _types["f32"])
+        ns = n if self._ms else 0
+        _check(_calls.adamw_step(n, self._bytes, self._p, g, code, self._m, self._v, self._ms, self._vs, self._state, self._copies,
+                                 (lr, betas[0], betas[1], eps, weight_decay, grad_scale), step, seed, live, stream, n, n, n, n, ns, ns,
+                                 n if self._copies else 0))
 
 
 def device_status(stream=None):

@@ -1,0 +1,330 @@
+// AdamW over lists of tensors: decoupled weight decay, states in fp32 or in 8 bits with a scale for each block of 128, optional bfloat16 copies of
+// the weights.  One launch takes up to kTensorsAtOnce tensors of any sizes.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "common.h"
+#include "eight_bit.h"
+
+namespace distdl {
+
+constexpr int kAdamThreads = 256;
+constexpr int kTileBlocks = 64;                          // blocks of 128 of a thread block's tile: 8192 elements
+constexpr int kTileElems = kTileBlocks * kScaleBlock;
+constexpr int kTensorsAtOnce = 320;
+
+struct AdamTensor {
+    float *p;
+    const void *g;
+    void *m, *v;
+    float *ms, *vs;
+    uint16_t *copy;
+    int64_t n;
+};
+struct AdamParams {
+    AdamTensor tensor[kTensorsAtOnce];
+    uint32_t first_tile[kTensorsAtOnce + 1];             // of each tensor, and behind the last
+    int32_t count, first_tensor;                         // tensors of this launch; number of its first one in the call
+    float beta1, one_beta1, beta2, one_beta2, eps, decay;
+    float log_beta1, log_beta2;
+    float lr_decay, grad_scale;
+    float rate, root;                                    // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    uint32_t seed, step;
+    const float *live;                                   // {lr, t, gradient scale} on the device, or null: what stands above
+};
+static_assert(sizeof(AdamParams) < 32700, "kernel parameters");
+
+// 32 well mixed bits of 32: multiplications by odd constants and shifted copies.
+__host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0xB504F333u;
+    x ^= x >> 15;
+    x *= 0x93CD3A2Du;
+    return x ^ (x >> 16);
+}
+
+// A magnitude up to 448 to an e4m3 value: floor(a / width + u) widths, width = distance of the e4m3 values at a, u in [0, 1) a multiple of 2^-16.  The
+// quotient is exact, the sum has at most the 24 bits of a float but for a carry's last one.
+__device__ __forceinline__ float stochastic_e4m3(float a, float u, bool never_zero) {
+    const uint32_t e = max(__float_as_uint(a) >> 23, 121u);                       // 2^-6 and below have one width
+    const float k = floorf(__fadd_rn(a * __uint_as_float((257u - e) << 23), u));  // 2^(3 - (e - 127))
+    return (never_zero && k == 0.f && a > 0.f ? 1.f : k) * __uint_as_float((e - 3u) << 23);
+}
+
+struct AdamStep {
+    float rate, root, decay, grad_scale;                 // decay: lr times the decay
+    uint32_t key;
+};
+
+template <bool EIGHT>
+__device__ __forceinline__ void adam_element(const AdamParams &P, const AdamStep &s, float &p, float g, float &m, float &v) {
+    g *= s.grad_scale;
+    m = fmaf(P.beta1, m, P.one_beta1 * g);
+    v = fmaf(P.beta2, v, P.one_beta2 * g * g);
+    const float r = sqrtf(v);
+    p -= fmaf(s.decay, p, __fdividef(s.rate * m, fmaf(r, s.root, P.eps)));        // the weight is rounded once
+    if (EIGHT) v = r;
+}
+
+// VEC: whole blocks by 16-byte accesses (the tensors' addresses are on 16-byte boundaries), half a warp a block.  The last elements of a
+// tensor go one by one.
+template <typename TG, bool EIGHT>
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_kernel(const __grid_constant__ AdamParams P) {
+    stream_enter();
+    int lo = 0, hi = P.count;                                                     // the tensor of this tile
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (P.first_tile[mid] <= blockIdx.x) lo = mid;
+        else hi = mid;
+    }
+    const AdamTensor &T = P.tensor[lo];
+    const int64_t tile0 = (int64_t)(blockIdx.x - P.first_tile[lo]) * kTileElems;
+    const int lane = threadIdx.x % kBlockLanes;
+    AdamStep s = {P.rate, P.root, P.lr_decay, P.grad_scale, 0u};
+    uint32_t step = P.step;
+    if (P.live) {
+        const float lr = P.live[0], t = P.live[1];
+        s.rate = lr / -expm1f(t * P.log_beta1);
+        s.root = rsqrtf(-expm1f(t * P.log_beta2));
+        s.decay = lr * P.decay;
+        s.grad_scale = P.live[2];
+        step = (uint32_t)t;
+    }
+    if (EIGHT) s.key = mixed(P.seed + step * 0x9E3779B9u) + (uint32_t)(P.first_tensor + lo) * 0xA54FF53Bu;
+    for (int b = threadIdx.x / kBlockLanes; b < kTileBlocks; b += kAdamThreads / kBlockLanes) {
+        const int64_t block0 = tile0 + (int64_t)b * kScaleBlock;
+        const int64_t warp0 = tile0 + (int64_t)(b & ~1) * kScaleBlock;            // both blocks of a warp walk together
+        if (warp0 >= T.n) break;
+        constexpr int VW = 4;
+        const int64_t at = block0 + lane * VW;
+        const int64_t left64 = T.n - at;
+        const int left = (int)max((int64_t)-1024, min(left64, (int64_t)1024));
+        const bool whole = block0 + kScaleBlock <= T.n;
+        float p[8], g[8], m[8], v[8];
+        Eight<float> raw;
+        Eight<TG> rawg;
+        const auto element = [&](int i) { return i / VW * (kBlockLanes * VW) + i % VW; };       // from `at`
+        if (whole) {
+            raw.template load<VW>(T.p + at, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = raw.get(i);
+            rawg.template load<VW>(reinterpret_cast<const TG *>(T.g) + at, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = rawg.get(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool there = element(i) < left;
+                p[i] = there ? T.p[at + element(i)] : 0.f;
+                g[i] = 0.f;
+                if (there) {
+                    if constexpr (sizeof(TG) == 4) g[i] = reinterpret_cast<const float *>(T.g)[at + element(i)];
+                    else g[i] = __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(T.g)[at + element(i)] << 16);
+                }
+            }
+        }
+        if constexpr (!EIGHT) {
+            float *tm = reinterpret_cast<float *>(T.m), *tv = reinterpret_cast<float *>(T.v);
+            if (whole) {
+                raw.template load<VW>(tm + at, left);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m[i] = raw.get(i);
+                raw.template load<VW>(tv + at, left);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = raw.get(i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    m[i] = element(i) < left ? tm[at + element(i)] : 0.f;
+                    v[i] = element(i) < left ? tv[at + element(i)] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) adam_element<false>(P, s, p[i], g[i], m[i], v[i]);
+            if (whole) {
+                raw.set(m);
+                raw.template store<VW>(tm + at, left);
+                raw.set(v);
+                raw.template store<VW>(tv + at, left);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (element(i) < left) tm[at + element(i)] = m[i], tv[at + element(i)] = v[i];
+            }
+        } else {
+            uint8_t *tm = reinterpret_cast<uint8_t *>(T.m), *tv = reinterpret_cast<uint8_t *>(T.v);
+            uint32_t cm[2] = {0u, 0u}, cv[2] = {0u, 0u};                          // four codes a word
+            if (whole) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    ld_bytes<4>(tm + at + r * kBlockLanes * VW, &cm[r]);
+                    ld_bytes<4>(tv + at + r * kBlockLanes * VW, &cv[r]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (element(i) < left) {
+                        cm[i / 4] |= (uint32_t)tm[at + element(i)] << (i % 4 * 8);
+                        cv[i / 4] |= (uint32_t)tv[at + element(i)] << (i % 4 * 8);
+                    }
+            }
+            const int64_t block = block0 / kScaleBlock;
+            const bool any = block0 < T.n;
+            const float sm = any ? T.ms[block] : 0.f, sv = any ? T.vs[block] : 0.f;
+            unpack_e4m3(cm[0], m);
+            unpack_e4m3(cm[1], m + 4);
+            unpack_e4m3(cv[0], v);
+            unpack_e4m3(cv[1], v + 4);
+            uint32_t topm = 0, topv = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                m[i] *= sm;
+                v[i] *= sv;
+                v[i] *= v[i];
+                adam_element<true>(P, s, p[i], g[i], m[i], v[i]);
+                if (element(i) >= left) m[i] = v[i] = 0.f;
+                topm = max(topm, __float_as_uint(m[i]) & 0x7fffffffu);
+                topv = max(topv, __float_as_uint(v[i]));
+            }
+            const BlockScale nm = block_scale(block_max(topm)), nv = block_scale(block_max(topv));
+            if (lane == 0 && any) T.ms[block] = nm.scale, T.vs[block] = nv.scale;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint64_t e = (uint64_t)(at + element(i));
+                const uint32_t bits = mixed((uint32_t)e * 0x9E3779B9u + (uint32_t)(e >> 32) * 0xA54FF53Bu + s.key);
+                const float a = fminf(fabsf(__fmul_rn(m[i], nm.inverse)), 448.f), b = fminf(__fmul_rn(v[i], nv.inverse), 448.f);
+                m[i] = copysignf(stochastic_e4m3(a, (float)(bits & 0xffffu) * 0x1p-16f, false), m[i]);
+                v[i] = stochastic_e4m3(b, (float)(bits >> 16) * 0x1p-16f, true);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                cm[r] = pack_e4m3(m[4 * r], m[4 * r + 1], m[4 * r + 2], m[4 * r + 3]);
+                cv[r] = pack_e4m3(v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]);
+            }
+            if (whole) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    st_bytes<4>(tm + at + r * kBlockLanes * VW, &cm[r]);
+                    st_bytes<4>(tv + at + r * kBlockLanes * VW, &cv[r]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (element(i) < left) {
+                        tm[at + element(i)] = (uint8_t)(cm[i / 4] >> (i % 4 * 8));
+                        tv[at + element(i)] = (uint8_t)(cv[i / 4] >> (i % 4 * 8));
+                    }
+            }
+        }
+        if (whole) {
+            raw.set(p);
+            raw.template store<VW>(T.p + at, left);
+            if (T.copy) {
+                Eight<bf16> c;
+                c.set(p);
+                c.template store<VW>(reinterpret_cast<bf16 *>(T.copy) + at, left);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (element(i) < left) {
+                    T.p[at + element(i)] = p[i];
+                    if (T.copy) T.copy[at + element(i)] = (uint16_t)pack_bf16(p[i], 0.f);
+                }
+        }
+    }
+}
+
+static bool rate_like(double v) { return std::isfinite(v) && v >= 0; }
+
+static distdl_status_t adamw_impl(int32_t count, const int64_t *elems, void *const *p, const void *const *g, distdl_dtype_t tg, void *const *m,
+                                  void *const *v, void *const *ms, void *const *vs, distdl_dtype_t state, void *const *copies, const double *hyper,
+                                  int64_t step, int64_t seed, const void *live, void *stream) {
+    const char *what = "adamw_step";
+    clear_error();
+    if (count < 0 || !hyper || (count > 0 && !elems)) return fail(DISTDL_ERR_INVALID_ARG, "%s: NULL argument or negative count", what);
+    if (count > DISTDL_MAX_TENSORS) return fail(DISTDL_ERR_UNSUPPORTED, "%s: more than %d tensors", what, DISTDL_MAX_TENSORS);
+    if (tg != DISTDL_F32 && tg != DISTDL_BF16) return fail(DISTDL_ERR_INVALID_ARG, "%s: gradients are F32 or BF16", what);
+    if (state != DISTDL_F32 && state != DISTDL_E4M3) return fail(DISTDL_ERR_INVALID_ARG, "%s: states are F32 or E4M3", what);
+    const double lr = hyper[0], beta1 = hyper[1], beta2 = hyper[2], eps = hyper[3], decay = hyper[4], scale = hyper[5];
+    if (!rate_like(lr) || !rate_like(decay) || !std::isfinite(scale)) return fail(DISTDL_ERR_INVALID_ARG, "%s: learning rate, decay or gradient scale", what);
+    if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1)) return fail(DISTDL_ERR_INVALID_ARG, "%s: betas lie in [0, 1)", what);
+    if (!std::isfinite(eps) || !((float)eps > 0)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a positive number", what);
+    if (step < 1 && !live) return fail(DISTDL_ERR_INVALID_ARG, "%s: steps are counted from 1", what);
+    const bool eight = state == DISTDL_E4M3;
+    if (count > 0 && (!p || !g || !m || !v || (eight && (!ms || !vs)))) return fail(DISTDL_ERR_INVALID_ARG, "%s: NULL argument", what);
+    const void *some = nullptr;
+    for (int i = 0; i < count; ++i) {
+        if (elems[i] < 0) return fail(DISTDL_ERR_INVALID_ARG, "%s: tensor %d has %lld elements", what, i, (long long)elems[i]);
+        if (elems[i] > (int64_t)1 << 40) return fail(DISTDL_ERR_UNSUPPORTED, "%s: tensor %d has more than 2^40 elements", what, i);
+        if (elems[i] == 0) continue;
+        const void *const need[6] = {p[i], g[i], m[i], v[i], eight ? ms[i] : p[i], eight ? vs[i] : p[i]};
+        for (const void *a : need) {
+            if (!a) return fail(DISTDL_ERR_INVALID_ARG, "%s: a buffer of tensor %d is NULL", what, i);
+            if (!aligned16(a)) return fail(DISTDL_ERR_ALIGNMENT, "%s: a buffer of tensor %d is not 16-byte aligned", what, i);
+        }
+        if (copies && copies[i] && !aligned16(copies[i])) return fail(DISTDL_ERR_ALIGNMENT, "%s: copies[%d] not 16-byte aligned", what, i);
+        some = p[i];
+    }
+    if (live && !aligned16(live)) return fail(DISTDL_ERR_ALIGNMENT, "%s: live not 16-byte aligned", what);
+    if (!some) return DISTDL_OK;
+    int device;
+    if (const distdl_status_t st = current_device(what, some, &device)) return st;
+
+    AdamParams P;
+    P.beta1 = (float)beta1;
+    P.one_beta1 = (float)(1 - beta1);
+    P.beta2 = (float)beta2;
+    P.one_beta2 = (float)(1 - beta2);
+    P.log_beta1 = (float)std::log(beta1);                        // beta = 0: minus infinity, and 1 - beta^t = 1
+    P.log_beta2 = (float)std::log(beta2);
+    P.eps = (float)eps;
+    P.decay = (float)decay;
+    P.lr_decay = (float)(lr * decay);
+    P.grad_scale = (float)scale;
+    P.rate = live ? 0.f : (float)(lr / (1 - std::pow(beta1, (double)step)));
+    P.root = live ? 0.f : (float)(1 / std::sqrt(1 - std::pow(beta2, (double)step)));
+    P.seed = (uint32_t)((uint64_t)seed ^ ((uint64_t)seed >> 32));
+    P.step = (uint32_t)step;
+    P.live = (const float *)live;
+    const auto launch = [&](uint32_t tiles) {
+        const auto with = [&](auto kernel) { launch_in_stream(kernel, dim3(tiles), dim3(kAdamThreads), 0, (cudaStream_t)stream, P); };
+        if (tg == DISTDL_F32) eight ? with(adamw_kernel<float, true>) : with(adamw_kernel<float, false>);
+        else eight ? with(adamw_kernel<bf16, true>) : with(adamw_kernel<bf16, false>);
+    };
+    P.count = 0;
+    P.first_tensor = 0;
+    P.first_tile[0] = 0;
+    for (int i = 0; i < count; ++i) {
+        const int64_t tiles = (elems[i] + kTileElems - 1) / kTileElems;
+        if (P.count == kTensorsAtOnce || (P.count > 0 && P.first_tile[P.count] + tiles > INT32_MAX)) {
+            if (P.first_tile[P.count]) launch(P.first_tile[P.count]);
+            P.first_tensor = i;
+            P.count = 0;
+        }
+        AdamTensor &T = P.tensor[P.count];
+        T.p = (float *)p[i];
+        T.g = g[i];
+        T.m = m[i];
+        T.v = v[i];
+        T.ms = eight ? (float *)ms[i] : nullptr;
+        T.vs = eight ? (float *)vs[i] : nullptr;
+        T.copy = copies ? (uint16_t *)copies[i] : nullptr;
+        T.n = elems[i];
+        P.first_tile[P.count + 1] = P.first_tile[P.count] + (uint32_t)tiles;
+        ++P.count;
+    }
+    if (P.first_tile[P.count]) launch(P.first_tile[P.count]);
+    DISTDL_CUDA_CHECK(cudaGetLastError());
+    return DISTDL_OK;
+}
+
+}  // namespace distdl
+
+extern "C" distdl_status_t distdl_adamw_step(int32_t count, const int64_t *elems, void *const *p, const void *const *g, distdl_dtype_t tg, void *const *m,
+                                             void *const *v, void *const *ms, void *const *vs, distdl_dtype_t state, void *const *copies,
+                                             const double *hyper, int64_t step, int64_t seed, const void *live, void *stream) {
+    return distdl::adamw_impl(count, elems, p, g, tg, m, v, ms, vs, state, copies, hyper, step, seed, live, stream);
+}

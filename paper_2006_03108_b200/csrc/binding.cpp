@@ -234,7 +234,7 @@ PyMethodDef methods[] = {
     FUNCTION(conv_fwd), FUNCTION(conv_adj), FUNCTION(conv_adj_params), FUNCTION(convg_fwd), FUNCTION(convg_adj), FUNCTION(convg_adj_params),
     FUNCTION(stencil3d_fwd), FUNCTION(stencil3d_adj), FUNCTION(pool_fwd), FUNCTION(pool_adj),
     FUNCTION(affine_fwd), FUNCTION(affine_adj), FUNCTION(affine_adj_params),
-    FUNCTION(quantize_rows), FUNCTION(quantize_weights), FUNCTION(rmsnorm_fwd), FUNCTION(rmsnorm_adj),
+    FUNCTION(quantize_rows), FUNCTION(quantize_weights), FUNCTION(rmsnorm_fwd), FUNCTION(rmsnorm_adj), FUNCTION(adamw_step),
     {"taps", taps, METH_O, nullptr},
     {"set_stream_lookup", (PyCFunction)(void (*)(void))set_stream_lookup, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -64,6 +64,15 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
     return (uint32_t)lo | (uint32_t)hi << 16;
 }
 
+__device__ __forceinline__ void unpack_e4m3(uint32_t codes, float *v) {      // exact
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(codes >> (16 * i))));
+        asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %2;\ncvt.f32.f16 %0, lo;\ncvt.f32.f16 %1, hi;\n}" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "r"(h));
+    }
+}
+
 // Accesses of B bytes to global memory.  Loads are coherent (a buffer may be worked on in place) and pass L1 by: every byte is read once.
 template <int B>
 __device__ __forceinline__ void ld_bytes(const void *p, uint32_t *v) {

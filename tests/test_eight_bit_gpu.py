@@ -269,3 +269,203 @@ def test_host_memory_is_refused():
     with pytest.raises(distdl.DistdlError) as e:
         distdl.quantize_rows(4, 128, 1, [t], [t.to(E4)], [torch.zeros(1, 4)])
     assert e.value.status == 1
+
+
+# ---------------------------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------------------------
+
+SIZES = [1, 3, 0, 127, 128, 129, 1000, 8192, 8193, 70001, 16384, 2, 257]
+HYPER = dict(lr=2e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, grad_scale=0.5)
+
+
+def adam_state(sizes, seed, eight):
+    p = [inputs.normal((n,), seed + 5 * i, 0.1) for i, n in enumerate(sizes)]
+    g = [inputs.normal((n,), seed + 5 * i + 1, 1e-2) for i, n in enumerate(sizes)]
+    m = [inputs.normal((n,), seed + 5 * i + 2, 1e-3) for i, n in enumerate(sizes)]
+    r = [np.abs(inputs.normal((n,), seed + 5 * i + 3, 4e-3)) for i, n in enumerate(sizes)]
+    if not eight:
+        return p, g, m, [a * a for a in r], None, None
+    m, ms = zip(*[o.moment_to_8_bits(a, 0.5, False) for a in m])
+    r, vs = zip(*[o.moment_to_8_bits(a, 0.5, True) for a in r])
+    return p, g, list(m), list(r), list(ms), list(vs)
+
+
+def adam_check(i, n, got, before, g, step, seed, eight, h=HYPER):
+    """One tensor after a step against fp64; got, before: (p, m, v, ms, vs)."""
+    p, m, v, ms, vs = before
+    m64, v64 = np.asarray(m, np.float64), np.asarray(v, np.float64)
+    if eight:
+        rep = lambda s: np.repeat(np.asarray(s, np.float64), 128)[:n]  # noqa: E731
+        m64, v64 = m64 * rep(ms), (v64 * rep(vs)) ** 2
+    b1, b2 = h["betas"]
+    c = h["grad_scale"]
+    pw, mw, vw = o.adamw(p, g, m64, v64, h["lr"], step, h["betas"], h["eps"], h["weight_decay"], c)
+    # m, v: the constants, the products and the sum are rounded; v's square doubles what it gets; p: its own rounding, and the change's
+    me = 5 * U * (b1 * np.abs(m64) + (1 - b1) * np.abs(c * g))
+    ve = 8 * U * vw
+    change = np.abs(h["lr"] * h["weight_decay"] * p) + np.abs(h["lr"] / (1 - b1 ** step) / (np.sqrt(vw / (1 - b2 ** step)) + h["eps"])) * (np.abs(mw) + me / (16 * U))
+    assert (np.abs(f64(got[0]) - pw) <= 1.01 * U * np.abs(pw) + 16 * U * change).all(), i
+    if not eight:
+        assert (np.abs(f64(got[1]) - mw) <= me).all() and (np.abs(f64(got[2]) - vw) <= ve).all(), i
+        return
+    bits = o.random_bits(0, n, seed, step, i)
+    for k, value, u, positive in ((1, mw, bits & 0xFFFF, False), (2, np.sqrt(vw), bits >> 16, True)):
+        code, scale = f64(got[k]), f64(got[k + 2])
+        pad = np.zeros(len(scale) * 128)
+        pad[:n] = value
+        top = np.maximum(np.abs(pad.reshape(-1, 128)).max(1), 2.0 ** -100)
+        assert (np.abs(scale - top / 448) <= 12 * U * top / 448).all(), i
+        a = np.minimum(np.abs(value) * 448 / np.repeat(top, 128)[:n], 448)
+        want = np.copysign(o.stochastic_e4m3(a, u / 65536.0, positive), value)
+        width = 2.0 ** (np.maximum(np.frexp(a)[1] - 1, -6) - 3.0)
+        # a code differs only where the value, known to 20 U, ends next to a random number: twice 20 U * 16 / 2^-16 of them or so
+        assert (np.abs(code - want) <= width * 1.0001).all() and (code != want).mean() <= 1e-3 + 2 / n, i
+        assert not positive or (code[vw > 0] > 0).all()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+@pytest.mark.parametrize("tg", [torch.float32, torch.bfloat16], ids=["gf32", "gbf16"])
+def test_adamw_against_the_definition(tg, eight):
+    p, g, m, v, ms, vs = adam_state(SIZES, 1000, eight)
+    g = [rounded(a, tg) for a in g]
+    out, held = Out(), E4 if eight else torch.float32
+
+    def put(a, dtype=torch.float32):
+        t = out(len(a), dtype=dtype)
+        t.copy_(dev(a))
+        return t
+
+    pd, md, vd = [put(a) for a in p], [put(a, held) for a in m], [put(a, held) for a in v]
+    msd, vsd = ([put(a) for a in ms], [put(a) for a in vs]) if eight else (None, None)
+    copies = [out(n, dtype=torch.bfloat16) if i % 3 else None for i, n in enumerate(SIZES)]
+    opt = distdl.AdamW(pd, md, vd, msd, vsd, copies)
+    gd = [dev(a, tg) for a in g]
+    for step in (7, 8):
+        before = [[f64(a[i]) if a is not None else None for a in (pd, md, vd, msd, vsd)] for i in range(len(SIZES))]
+        opt.step(gd, step=step, seed=99, **HYPER)
+        for i, n in enumerate(SIZES):
+            if n:
+                adam_check(i, n, [a[i] if a is not None else None for a in (pd, md, vd, msd, vsd)], before[i], g[i].astype(np.float64), step, 99, eight)
+            if copies[i] is not None:
+                assert torch.equal(copies[i], pd[i].bfloat16())
+    assert all(torch.equal(a, dev(b, tg)) for a, b in zip(gd, g))
+    out.check()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+def test_adamw_of_many_tensors_is_that_of_each(eight):
+    """More tensors than a launch takes: the same bits as one at a time (in 8 bits: up to the random numbers, which go by the tensor)."""
+    sizes = [(17 * i) % 300 for i in range(701)]
+    p, g, m, v, ms, vs = adam_state(sizes, 7000, eight)
+    held = E4 if eight else torch.float32
+    state = lambda: [[dev(a) for a in p], [dev(a, held) for a in m], [dev(a, held) for a in v]] + ([[dev(a) for a in ms], [dev(a) for a in vs]] if eight else [])  # noqa: E731
+    a, b, gd = state(), state(), [dev(x) for x in g]
+    distdl.AdamW(*a).step(gd, step=3, **HYPER)
+    for i in range(len(sizes)):
+        distdl.AdamW(*[x[i:i + 1] for x in b]).step(gd[i:i + 1], step=3, **HYPER)
+    for k in (0, 3, 4) if eight else (0, 1, 2):
+        assert all(torch.equal(x, y) for x, y in zip(a[k], b[k])), k
+    if eight:
+        i = 653                                                      # in the third launch
+        adam_check(i, sizes[i], [x[i] for x in a], [p[i], m[i], v[i], ms[i], vs[i]], g[i].astype(np.float64), 3, 0, True)
+
+
+def test_adamw_first_step_moves_every_weight_by_the_rate():
+    """From a state of zeros: |change| = lr for every gradient that is not zero, whatever its size; nothing else moves."""
+    n = 1000
+    g = inputs.normal((n,), 3) * np.float32(10.0) ** inputs.integers((n,), 4, -6, 7)
+    g[::7] = 0.0
+    for eight in (False, True):
+        p = torch.zeros(n, device=DEV)
+        m, v = [torch.zeros(n, device=DEV, dtype=E4 if eight else torch.float32) for _ in range(2)]
+        scales = [[torch.zeros(8, device=DEV)] for _ in range(2)] if eight else [None, None]
+        distdl.AdamW([p], [m], [v], *scales).step([dev(g)], 1e-2, 1, eps=1e-30, weight_decay=0.0)
+        assert (np.abs(np.abs(f64(p)) - 1e-2 * (g != 0)) <= 1e-2 * 16 * U).all() and (np.sign(f64(p)) == -np.sign(g)).all()
+
+
+def test_adamw_states_in_8_bits_follow_small_decays():
+    """A second moment that shrinks by 0.1 % a step does shrink: the codes' mean over 4096 elements after 400 steps without gradients
+    (e4m3 steps are 6 to 12 %: rounded to nearest nothing would move), and a first moment at 0.5 % a step."""
+    n, steps = 4096, 400
+    p, g = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    m, v = [torch.full((n,), 300.0, device=DEV).to(E4) for _ in range(2)]
+    ms, vs = [torch.ones(n // 128, device=DEV) for _ in range(2)]
+    m[::128] = v[::128] = 448.0                                       # holds the scale of its block, which decays with it
+    opt = distdl.AdamW([p], [m], [v], [ms], [vs])
+    start = [(a.double() * s.double().repeat_interleave(128)).mean().item() for a, s in ((m, ms), (v, vs))]
+    for t in range(steps):
+        opt.step([g], 1e-3, 10 + t, betas=(0.995, 0.999))
+    end = [(a.double() * s.double().repeat_interleave(128)).mean().item() for a, s in ((m, ms), (v, vs))]
+    # each rounding keeps the mean and moves a code by less than 1/8 of itself: after 400 of them the deviation of an element is at most
+    # 1/16 sqrt(400) of itself, of the mean of 4096 elements 1.25 / 64 -- the scales are exact but for their roundings
+    assert abs(end[0] / start[0] / 0.995 ** steps - 1) < 0.1 and abs(end[1] / start[1] / 0.999 ** (steps / 2) - 1) < 0.1
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+def test_adamw_live_arguments_and_replayed_steps(eight):
+    p, g, m, v, ms, vs = adam_state([5000, 300], 500, eight)
+    held = E4 if eight else torch.float32
+    state = lambda: [[dev(a) for a in p], [dev(a, held) for a in m], [dev(a, held) for a in v]] + ([[dev(a) for a in ms], [dev(a) for a in vs]] if eight else [])  # noqa: E731
+    gd = [dev(a) for a in g]
+    h = {k: x for k, x in HYPER.items() if k not in ("lr", "grad_scale")}
+    live = torch.zeros(3, device=DEV)
+    eager, other, replayed = state(), state(), state()
+    opts = [distdl.AdamW(*s) for s in (eager, other, replayed)]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        live.copy_(torch.tensor([0.0, 1.0, 0.0]))
+        distdl.AdamW(*state()).step(gd, 0.0, 0, live=live, seed=3, **h)       # loads the kernel
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        opts[2].step(gd, 0.0, 0, live=live, seed=3, **h)
+    torch.cuda.synchronize()
+    for t in (1, 2, 3, 1000):
+        live.copy_(torch.tensor([1e-3 * t, float(t), 0.25]))
+        opts[0].step(gd, 0.0, 0, live=live, seed=3, **h)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        opts[1].step(gd, 1e-3 * t, t, seed=3, grad_scale=0.25, **h)
+    for a, b in zip(eager, replayed):
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
+    for a, b in zip(eager[0], other[0]):                                # 1 - beta^t in fp32 and fp64
+        assert (a - b).abs().max() <= 64 * U * (0.2 + 4 * 1.1)
+
+
+def test_adamw_bad_gradients_stay_where_they_are():
+    n = 1024
+    for eight in (False, True):
+        p, g, m, v, ms, vs = adam_state([n], 800, eight)
+        g[0][5], g[0][600] = np.inf, np.nan
+        held = E4 if eight else torch.float32
+        s = [[dev(a) for a in p], [dev(a, held) for a in m], [dev(a, held) for a in v]] + ([[dev(a) for a in ms], [dev(a) for a in vs]] if eight else [])
+        distdl.AdamW(*s).step([dev(g[0])], step=4, **HYPER)
+        touched = np.isin(np.arange(n) // (128 if eight else 1), [0, 4] if eight else [5, 600])
+        value = [f64(s[0][0])]
+        assert np.isnan(value[0][600]) and np.isfinite(value[0][~np.isin(np.arange(n), [5, 600])]).all()
+        for k in (1, 2):
+            x = f64(s[k][0]) * (np.repeat(f64(s[k + 2][0]), 128) if eight else 1.0)
+            assert np.isfinite(x[~touched]).all() and not np.isfinite(x[touched]).any()
+
+
+def test_adamw_beyond_32_bits_of_elements():
+    n, tail = 2 ** 32 + 333, 1000
+    if torch.cuda.get_device_properties(0).total_memory < 80 << 30:
+        pytest.skip("needs 40 GB")
+    p, g = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV, dtype=torch.bfloat16)
+    m, v = [torch.zeros(n, device=DEV, dtype=torch.uint8).view(E4) for _ in range(2)]
+    ms, vs = [torch.zeros(-(-n // 128), device=DEV) for _ in range(2)]
+    at = (n - tail) // 128 * 128
+    pw, gw = inputs.normal((n - at,), 1), rounded(inputs.normal((n - at,), 2), torch.bfloat16)
+    p[at:].copy_(dev(pw))
+    g[at:].copy_(dev(gw))
+    distdl.AdamW([p], [m], [v], [ms], [vs]).step([g], step=2, seed=5, **HYPER)
+    zero = np.zeros(n - at)
+    _, mw, vw = o.adamw(pw, gw, zero, zero, HYPER["lr"], 2, HYPER["betas"], HYPER["eps"], HYPER["weight_decay"], HYPER["grad_scale"])
+    bits = o.random_bits(at, n - at, 5, 2, 0)
+    for code, scale, value, u, positive in ((m, ms, mw, bits & 0xFFFF, False), (v, vs, np.sqrt(vw), bits >> 16, True)):
+        want, sw = o.moment_to_8_bits(value, u / 65536.0, positive)
+        assert (f64(code[at:]) != want).mean() <= 3e-3 and np.allclose(f64(scale[at // 128:]), sw, rtol=12 * U)
+    assert not p[:at].any() and not m.view(torch.uint8)[:at].any() and p[at:].ne(dev(pw)).any()

@@ -176,3 +176,58 @@ def test_python_calls_refuse_lists_types_sizes_and_layouts():
     refused(2, distdl.rmsnorm_adj, 4, 256, 2, x, None, x, gamma, t(4), q, None, t(1 << 20))
     if not torch.cuda.is_available():
         refused(5, distdl.quantize_rows, 4, 256, 2, x, q, s)          # no device: nothing runs, and says so
+
+
+def test_adamw_refusals():
+    lib, a, odd = distdl.lib(), _array(5000), _array(4, first=0x10004)
+    n4 = (ctypes.c_int64 * 4)(8, 0, 130, 8)
+    good = (1e-3, 0.9, 0.999, 1e-8, 0.1, 1.0)
+
+    def step(count=4, elems=n4, p=a, g=a, tg=distdl.F32, m=a, v=a, ms=a, vs=a, state=distdl.E4M3, copies=a, hyper=good, t=1, live=None):
+        h = None if hyper is None else (ctypes.c_double * 6)(*hyper)
+        return lib.distdl_adamw_step(count, elems, p, g, tg, m, v, ms, vs, state, copies, h, t, 0, live, None)
+
+    assert step(count=-1) == 1 and step(hyper=None) == 1 and step(elems=None) == 1 and step(count=5000, elems=(ctypes.c_int64 * 5000)()) == 4
+    assert step(tg=distdl.F64) == 1 and step(tg=distdl.E4M3) == 1 and step(state=distdl.BF16) == 1
+    for k, bad in ((0, -1.0), (0, float("nan")), (0, float("inf")), (1, 1.0), (1, -0.1), (2, 1.0), (2, float("nan")), (3, 0.0), (3, 1e-60), (4, -0.1), (5, float("inf"))):
+        assert step(hyper=good[:k] + (bad,) + good[k + 1:]) == 1, (k, bad)
+    assert step(t=0) == 1 and step(t=-3) == 1 and step(elems=(ctypes.c_int64 * 4)(8, -1, 8, 8)) == 1 and step(elems=(ctypes.c_int64 * 4)(8, 1 << 41, 8, 8)) == 4
+    hole = (vp * 4)(0x10000, None, 0x30000, None)
+    for name in ("p", "g", "m", "v", "ms", "vs"):
+        assert step(**{name: None}) == 1 and step(**{name: hole}) == 1 and step(**{name: odd}) == 3, name
+    assert step(copies=odd) == 3 and step(live=vp(0x10004)) == 3
+    assert step(count=0) == 0 and step(elems=(ctypes.c_int64 * 4)()) == 0             # nothing to do
+
+
+def test_adamw_handle_refuses_tensors_that_do_not_belong_together():
+    t = lambda *shape, dtype=torch.float32: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    e4 = torch.float8_e4m3fn
+    p = [t(300), t(5)]
+    m8 = lambda: [t(300, dtype=e4), t(5, dtype=e4)]  # noqa: E731
+    sc = lambda: [t(3), t(1)]  # noqa: E731
+    f = lambda: [t(300), t(5)]  # noqa: E731
+
+    def refused(status, *args):
+        with pytest.raises(distdl.DistdlError) as e:
+            distdl.AdamW(*args)
+        assert e.value.status == status
+
+    refused(1, p, f()[:1], f())
+    refused(2, p, [t(300), t(6)], f())
+    refused(2, p, f(), m8())
+    refused(1, p, m8(), m8())
+    refused(1, p, m8(), m8(), sc(), None)
+    refused(2, p, m8(), m8(), [t(2), t(1)], sc())
+    refused(2, p, f(), f(), None, None, [t(300), None])
+    refused(2, [t(600)[::2], t(5)], f(), f())
+    refused(1, p, [p[0], t(5)], f())                                                   # one buffer in two places
+    both = t(600)
+    refused(1, p, [both[:300], t(5)], [both[299:599], t(5)])
+    opt = distdl.AdamW(p, f(), f(), None, None, [None, t(5, dtype=torch.bfloat16)])
+    for g in ([t(300)], [t(300), t(6)], [t(300), t(5, dtype=torch.bfloat16)], [t(2, 300)[:, ::2], t(5)]):
+        with pytest.raises(distdl.DistdlError):
+            opt.step(g, 1e-3, 1, stream=0)
+    with pytest.raises(distdl.DistdlError) as e:
+        opt.step(f(), 1e-3, 0, stream=0)
+    assert e.value.status == 1
+    distdl.AdamW([], [], []).step([], 1e-3, 1)
