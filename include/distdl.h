@@ -497,6 +497,30 @@ distdl_status_t distdl_rmsnorm_adj(int64_t nb, int64_t nf, int32_t pf, const voi
                                    int64_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Affine layer in 8 bits on a Pfo x Pfi worker grid (Section 4, "Dense layers": the forward and adjoint affine algorithms, as
+ * affine_fwd and affine_adj), activations and weights as quantize_rows and quantize_weights leave them.
+ *
+ * affine_fp8_fwd: y_i = R over j = 0..Pfi-1 in order of  x_j W_ij^T  (+ bias_i)
+ * affine_fp8_adj: dx_j = R over i = 0..Pfo-1 in order of  dy_i W_ij
+ * x[j]  E4M3 [nb, nfi/Pfi]      xs[j]  F32 [ceil((nfi/Pfi)/128)][nb]
+ * w[i*Pfi+j] E4M3 [nfo/Pfo, nfi/Pfi]   ws[i*Pfi+j] F32 [ceil((nfo/Pfo)/128)][ceil((nfi/Pfi)/128)]
+ * y[i]  [nb, nfo/Pfo] of type t (F32 or BF16)      bias[i] F32 [nfo/Pfo] or NULL, or bias == NULL
+ * dy[i] E4M3 [nb, nfo/Pfo], dys[i] F32 [ceil((nfo/Pfo)/128)][nb];   dx[j] [nb, nfi/Pfi] of type t
+ * Products of 128 of the contraction are added up by the tensor cores in fp32; each is then multiplied with its two scales (their
+ * product is taken in fp32) and added to an fp32 sum, in the workers' and blocks' order -- in up to eight runs of that order, whose
+ * sums are added up in order, where one run would leave SMs idle.  Rounded once, to t, with the bias.
+ * nfi % Pfi == 0, nfo % Pfo == 0 (else DISTDL_ERR_SHAPE); the per-worker block sizes must be multiples of 16, Pfo, Pfi <= 8 and
+ * Pfo * Pfi <= 16 (else DISTDL_ERR_UNSUPPORTED); 1 <= nb <= 2^20.  dW and db: distdl_affine_adj_params on the bfloat16 values.
+ * A launch whose device-side waits ran out reports through distdl_device_status().
+ * ---------------------------------------------------------------------- */
+distdl_status_t distdl_affine_fp8_fwd(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *x,
+                                      const void *const *xs, const void *const *w, const void *const *ws,
+                                      const void *const *bias, distdl_dtype_t t, void *const *y, void *stream);
+distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *dy,
+                                      const void *const *dys, const void *const *w, const void *const *ws,
+                                      distdl_dtype_t t, void *const *dx, void *stream);
+
+/* ------------------------------------------------------------------------
  * AdamW over `count` tensors at once: the step from the gradients of the *_adj_params calls to new weights (an addition of
  * this library).  For every element, with the gradient g scaled by c:
  *     m = beta1 m + (1 - beta1) c g;   v = beta2 v + (1 - beta2) (c g)^2;

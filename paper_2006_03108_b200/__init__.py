@@ -100,6 +100,8 @@ def lib():
     L.distdl_rmsnorm_fwd.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, vp, c_i32, pvp, pvp, pvp, pvp, vp, vp]
     L.distdl_rmsnorm_adj_workspace.argtypes = [c_i64, c_i64, c_i32, pi64]
     L.distdl_rmsnorm_adj.argtypes = [c_i64, c_i64, c_i32, pvp, pvp, pvp, pvp, vp, c_i32, c_i32, pvp, pvp, vp, c_i64, vp]
+    L.distdl_affine_fp8_fwd.argtypes = [c_i64, c_i64, c_i64, c_i32, c_i32, pvp, pvp, pvp, pvp, pvp, c_i32, pvp, vp]
+    L.distdl_affine_fp8_adj.argtypes = [c_i64, c_i64, c_i64, c_i32, c_i32, pvp, pvp, pvp, pvp, c_i32, pvp, vp]
     L.distdl_adamw_step.argtypes = [c_i32, pi64, pvp, pvp, c_i32, pvp, pvp, pvp, pvp, c_i32, pvp, vp, c_i64, c_i64, vp, vp]
     L.distdl_device_status.argtypes = [vp]
     L.distdl_selftest_wait_timeout.argtypes = [c_i64, vp]
@@ -628,6 +630,34 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
     _need("dgamma", dgamma, pf, bf, f32)
     _check((_calls or _load()).rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
                                            workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
+
+
+def _need_fp8(what, nb, nfi, nfo, pfo, pfi, act, scales, nact, blk, w, ws, out, nout, blk_out, dtype):
+    e4m3, f32 = _types["e4m3"], _types["f32"]
+    bfi, bfo = nfi // pfi, nfo // pfo
+    _need(what[0], act, nact, nb * blk, e4m3)
+    _need(what[1], scales, nact, nb * _blocks128(blk), f32)
+    _need("w", w, pfo * pfi, bfo * bfi, e4m3)
+    _need("ws", ws, pfo * pfi, _blocks128(bfo) * _blocks128(bfi), f32)
+    _need(what[2], out, nout, nb * blk_out, dtype)
+
+
+def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
+    """y_i = sum over j of x_j W_ij^T (+ bias_i) with x, xs as quantize_rows and w, ws as quantize_weights leave them; y float32 or bfloat16."""
+    code, dtype = _float_code("y", y)
+    bfi, bfo = _features("affine_fp8_fwd", nfi, pfi), _features("affine_fp8_fwd", nfo, pfo)
+    _need_fp8(("x", "xs", "y"), nb, nfi, nfo, pfo, pfi, x, xs, pfi, bfi, w, ws, y, pfo, bfo, dtype)
+    if bias is not None:
+        _need("bias", [b for b in bias if b is not None], 0, bfo, _types["f32"])
+    _check((_calls or _load()).affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, code, y, stream, pfi, pfi, pfo * pfi, pfo * pfi, pfo, pfo))
+
+
+def affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, dx, stream=None):
+    """dx_j = sum over i of dy_i W_ij with dy, dys as quantize_rows and w, ws as quantize_weights leave them; dx float32 or bfloat16."""
+    code, dtype = _float_code("dx", dx)
+    bfi, bfo = _features("affine_fp8_adj", nfi, pfi), _features("affine_fp8_adj", nfo, pfo)
+    _need_fp8(("dy", "dys", "dx"), nb, nfi, nfo, pfo, pfi, dy, dys, pfo, bfo, w, ws, dx, pfi, bfi, dtype)
+    _check((_calls or _load()).affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, code, dx, stream, pfo, pfo, pfo * pfi, pfo * pfi, pfi))
 
 
 class AdamW:

@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libdistdl.so")
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))    # the calls from Python, an extension of this interpreter
 
 SOURCES = ["planner.cpp", "partition.cu", "bcast_reduce.cu", "halo.cu", "convd.cu", "convg.cu", "pool.cu", "stencil3d.cu", "affine.cu",
-           "quantize.cu", "rmsnorm.cu", "adamw.cu"]
+           "quantize.cu", "rmsnorm.cu", "adamw.cu", "affine_fp8.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

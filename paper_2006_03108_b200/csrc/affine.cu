@@ -22,6 +22,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "tcgen05.h"
 #include "tma.h"
 
 namespace distdl {
@@ -50,52 +51,15 @@ struct AffineParams {
 // ------------------------------------------------------------------------------------------
 // PTX wrappers
 // ------------------------------------------------------------------------------------------
-// Bounded wait: false if the limit ran out or another role already gave up.  The limit is counted
-// in SM clock cycles (reading %globaltimer costs several hundred nanoseconds, which would serialise
-// the pipeline when it sits on the critical path of every k-block), and the clock is only looked
-// at once in a while.
-constexpr long long kWaitLimitCycles = 4000000000ll;   // about 2 s
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag,
-                                          long long limit_cycles = kWaitLimitCycles) {
-    long long t0 = 0;
-    for (unsigned spins = 0;; ++spins) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((spins & 63u) == 63u) {
-            if (*abort_flag) return false;
-            const long long now = clock64();
-            if (t0 == 0) t0 = now;
-            if (now - t0 > limit_cycles) {
-                *abort_flag = 1;
-                atomicExch(&g_affine_status, (int)DISTDL_ERR_TIMEOUT);
-                return false;
-            }
-        }
-    }
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit_cycles = kWaitLimitCycles) {
+    return bounded_wait(bar, parity, abort_flag, &g_affine_status, limit_cycles);
 }
-__device__ __forceinline__ void tcgen05_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n.reg .pred p;\n"
         "setp.ne.b32 p, %4, 0;\n"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
         ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-
-// Shared-memory matrix descriptor, 128-byte swizzle.  Fields (bit positions): start address >> 4
-// [0,14), leading byte offset >> 4 [16,30), stride byte offset >> 4 [32,46), descriptor version 1
-// [46,48), layout type 2 = 128-byte swizzle [61,64).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr >> 4) & 0x3FFF);
-    d |= (uint64_t)((lbo_bytes >> 4) & 0x3FFF) << 16;
-    d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFF) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
 }
 
 // Instruction descriptor of kind::f16: D = fp32 [4,6) = 1, A = B = bf16 [7,10) = [10,13) = 1,
@@ -105,28 +69,6 @@ __host__ __device__ constexpr uint32_t instr_desc(int m, int n, int b_mn_major) 
            ((uint32_t)(m >> 4) << 24);
 }
 
-// ------------------------------------------------------------------------------------------
-// Cluster helpers for the two-SM variant
-// ------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, uint32_t bar_cluster_addr) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar_cluster_addr) : "memory");
-}
 __device__ __forceinline__ void tcgen05_commit_pair(uint32_t bar) {
     const uint16_t mask = 3;   // both blocks of the pair
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
@@ -361,21 +303,6 @@ struct AffineSplitParams {
     int32_t stages, stage_bytes;
 };
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *v) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
 __global__ void __launch_bounds__(kAffineThreads, 1)
 affine_kernel_split(const __grid_constant__ AffineSplitParams Q) {
     const AffineParams &P = Q.p;
@@ -557,29 +484,12 @@ constexpr int kQuadBufBytes = kTileM * kQuadPitch * 4;      // 67,584
 static_assert(3 * kQuadBufBytes <= kQuadStages * kQuadStageBytes, "epilogue buffers must fit in the ring");
 static_assert(kQuadBufBytes % 16 == 0, "bulk copies move multiples of 16 bytes");
 
-__device__ __forceinline__ void tcgen05_commit_mask(uint32_t bar, uint16_t mask) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"(mask) : "memory");
-}
 // shared memory of this block -> shared memory of another block of the cluster; the bytes are
 // counted on a barrier of the destination block
 __device__ __forceinline__ void bulk_copy_to_cta(uint32_t dst_cluster_addr, uint32_t src, uint32_t bytes, uint32_t bar_cluster_addr) {
     asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst_cluster_addr), "r"(src), "r"(bytes), "r"(bar_cluster_addr) : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *v) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
-          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-        : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
 __global__ void __launch_bounds__(kQuadThreads, 1)
 affine_kernel_quad(const __grid_constant__ AffineParams P) {
     extern __shared__ uint8_t smem_raw[];
@@ -811,9 +721,6 @@ struct AffineDwParams {
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int32_t c0, int32_t c1) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // barrier 1 of the four epilogue warps, combined with an AND over their predicates
 __device__ __forceinline__ bool epilogue_all(bool pred) {
@@ -1311,6 +1218,7 @@ extern "C" distdl_status_t distdl_affine_adj_params(int64_t nb, int64_t nfi, int
 
 namespace distdl {
 int conv_take_status();   // convd.cu
+int fp8_take_status();    // affine_fp8.cu
 
 // Self-test of the bounded wait: one thread waits, through the same mbar_wait as the kernels above, on a
 // barrier that nobody arrives at.  The wait gives up after `limit_cycles`, records DISTDL_ERR_TIMEOUT in the
@@ -1348,10 +1256,10 @@ extern "C" distdl_status_t distdl_device_status(void *stream) {
         const int zero = 0;
         DISTDL_CUDA_CHECK(cudaMemcpyToSymbol(g_affine_status, &zero, sizeof(int)));
     }
-    const int cst = conv_take_status();
-    if (cst < 0) return fail(DISTDL_ERR_CUDA, "device_status: reading the status word failed");
-    if (st != 0 || cst != 0)
+    const int cst = conv_take_status(), fst = fp8_take_status();
+    if (cst < 0 || fst < 0) return fail(DISTDL_ERR_CUDA, "device_status: reading the status word failed");
+    if (st != 0 || cst != 0 || fst != 0)
         return fail(DISTDL_ERR_TIMEOUT, "a bounded device-side wait of %s kernel ran out",
-                    st != 0 ? "an affine" : "a convolution");
+                    st != 0 || fst != 0 ? "an affine" : "a convolution");
     return DISTDL_OK;
 }

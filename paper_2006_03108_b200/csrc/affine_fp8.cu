@@ -1,0 +1,748 @@
+// Distributed affine layer on a Pfo x Pfi worker grid with activations and weights in 8 bits (e4m3 values with a scale for each 1 x 128 of a sample and
+// each 128 x 128 of a weight block): forward  y_i = R_j (x_j W_ij^T) (+ b_i)  and adjoint  dx_j = R_i (dy_i W_ij).
+//
+// B and R are as in the bfloat16 layer (affine.cu): blocks of x are read through L2, and R goes on in the accumulator in worker order.  The scales change
+// every 128 of the contraction, on both sides, so a product of 128 is all that the tensor cores may add up by themselves: it is finished in tensor memory,
+// and the epilogue warps add it, times its two scales, to sums in their registers, while the next 128 are multiplied into the other half of tensor memory.
+// The sums are fp32 throughout, in the order of the k-blocks.
+//
+// The forward pass takes the weights as the K-major operand, the adjoint takes the same bytes as the MN-major one; a scale block is 128 x 128, so both
+// read the same scales.  Every wait is bounded, as in affine.cu.
+#include <cuda.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "common.h"
+#include "eight_bit.h"
+#include "tcgen05.h"
+#include "tma.h"
+
+namespace distdl {
+
+constexpr int kF8K = 128;                                   // of the contraction at a time: one scale, one 128-byte swizzle row
+constexpr int kF8Rows = 128;                                // rows of a thread block's tile
+constexpr int kF8Threads = 384;                             // warp 0: TMA, warp 1: MMA and tensor memory, warps 4..11: sums
+constexpr int kF8MaxWorkers = 16;
+
+__device__ int g_fp8_status = 0;                            // 0 or DISTDL_ERR_TIMEOUT
+int fp8_take_status() {
+    int st = 0;
+    if (cudaMemcpyFromSymbol(&st, g_fp8_status, sizeof(int)) != cudaSuccess) return -1;
+    if (st) {
+        const int zero = 0;
+        cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(int));
+    }
+    return st;
+}
+
+struct AffineF8Params {
+    CUtensorMap a_map[8];                                   // activation blocks (x_j forward, dy_i adjoint)
+    CUtensorMap w_map[kF8MaxWorkers];                       // weight blocks, worker order i * pfi + j
+    const float *as[8];                                     // scales of the activations [k-blocks][nb]
+    const float *ws[kF8MaxWorkers];                         // scales of the weights
+    void *out[8];
+    const float *bias[8];
+    int32_t nb, pfi;
+    int32_t blk_out, blk_red;                               // columns of an output block, contraction inside one worker
+    int32_t nred;                                           // workers summed over
+    int32_t kpw;                                            // k-blocks of a worker
+    int32_t ws_k, ws_n;                                     // steps in the weights' scales: to the next k-block, the next 128 columns
+    int32_t adjoint, out_bf16;
+};
+
+__device__ __forceinline__ bool f8_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    return bounded_wait(bar, parity, abort_flag, &g_fp8_status, kWaitLimitCycles);
+}
+// kind::f8f6f4, K = 32: both operands e4m3 (formats 0), D = fp32
+__device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Instruction descriptor: D = fp32 [4,6) = 1, A = B = e4m3 [7,10) = [10,13) = 0, A major bit 15, B major bit 16 (1 = MN-major), N >> 3 in [17,23),
+// M >> 4 in [24,29).
+__host__ __device__ constexpr uint32_t f8_instr(int m, int n, int a_mn, int b_mn) {
+    return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+}
+// acc += s * d for pairs of floats
+__device__ __forceinline__ void fma_pair(uint64_t &acc, uint64_t s, uint64_t d) {
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(s), "l"(d));
+}
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+// 32 columns of tensor memory, in pairs
+__device__ __forceinline__ void tmem_ld32_pairs(uint32_t taddr, uint64_t *d) {
+    uint32_t v[32];
+    tmem_ld32(taddr, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) d[i] = (uint64_t)v[2 * i] | (uint64_t)v[2 * i + 1] << 32;
+}
+
+// Walks through the scales of one row of the activations and one block of columns of the weights, k-block by k-block, worker by worker.
+struct ScaleWalk {
+    const AffineF8Params &P;
+    int r, kin, oblk, row, nblk;
+    const float *a, *w;
+    bool row_there, col_there;
+    __device__ __forceinline__ ScaleWalk(const AffineF8Params &p, int kb, int oblk_, int row_, int col)
+        : P(p), r(kb / p.kpw), kin(kb - kb / p.kpw * p.kpw), oblk(oblk_), row(row_), nblk(col / kScaleBlock), row_there(row_ < p.nb), col_there(col < p.blk_out) {
+        seek();
+    }
+    __device__ __forceinline__ void seek() {
+        if (r < P.nred) {
+            a = P.as[r] + (int64_t)kin * P.nb + row;
+            w = P.ws[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r] + (int64_t)kin * P.ws_k + (int64_t)nblk * P.ws_n;
+        }
+    }
+    __device__ __forceinline__ float next() {
+        float s = 0.f;
+        if (r < P.nred && row_there && col_there) s = __ldg(a) * __ldg(w);
+        a += P.nb;
+        w += P.ws_k;
+        if (++kin == P.kpw) {
+            kin = 0;
+            ++r;
+            seek();
+        }
+        return s;
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Batches over 128: a pair of blocks owns a 256 x TN tile (cta_group::2, 128 rows and half of the weights' columns each); a cluster of S pairs shares the
+// k-blocks of a tile, in S runs one after the other, and adds up the S sums through distributed shared memory in that order.
+// ------------------------------------------------------------------------------------------
+constexpr int kF8Tail = 1024 + 256;                         // alignment, barriers
+template <int TN>
+struct F8Cfg {
+    static constexpr int kABytes = kF8Rows * kF8K;          // 16 KB
+    static constexpr int kBBytes = TN / 2 * kF8K;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = 196608 / kStageBytes;    // 6 or 8
+    static constexpr int kPitch = TN + 4;                   // floats of a row of sums in shared memory; spreads rows over the banks
+    static constexpr int kSmemBytes = kStages * kStageBytes + kF8Tail;
+    static_assert(kF8Rows * kPitch * 4 <= kStages * kStageBytes, "the sums take the ring's place");
+    static_assert((2 * kStages + 4) * 8 + 8 <= 256, "barriers");
+    static_assert(kStages >= 2, "");
+};
+
+template <int TN>
+__global__ void __launch_bounds__(kF8Threads, 1)
+affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
+    stream_enter();
+    using C = F8Cfg<TN>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;           // the swizzle is a function of address bits [7,10)
+    uint8_t *aligned = smem_raw + (base - raw);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + C::kStages * C::kStageBytes);
+    const uint32_t bar_full = smem_u32(bars);
+    const uint32_t bar_empty = bar_full + 8 * C::kStages;
+    const uint32_t bar_done = bar_empty + 8 * C::kStages;   // two: a product of 128 is in tensor memory
+    const uint32_t bar_free = bar_done + 16;                // two: it has been taken
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * C::kStages + 4);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t crank = cluster_ctarank(), prank = crank & 1, leader = crank & ~1u;
+    uint32_t cluster_size;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(cluster_size));
+    const int splits = (int)cluster_size / 2, split = (int)crank / 2;
+    const int tile = (int)(blockIdx.x / cluster_size);
+    const int row_tiles = (P.nb + 2 * kF8Rows - 1) / (2 * kF8Rows);
+    const int m0 = (tile % row_tiles) * 2 * kF8Rows + (int)prank * kF8Rows;
+    const int tiles_per_block = (P.blk_out + TN - 1) / TN;
+    const int oblk = tile / row_tiles / tiles_per_block;
+    const int n0 = (tile / row_tiles - oblk * tiles_per_block) * TN;
+    const int all = P.nred * P.kpw;
+    const int kb0 = (int)((int64_t)all * split / splits), kb1 = (int)((int64_t)all * (split + 1) / splits);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar_done + 8 * b, 1);
+            mbar_init(bar_free + 8 * b, 16);                // the summing warps of both blocks
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)(2 * TN)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    cluster_sync_all();
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // 256 columns: a summing thread holds 128 sums.  The launch gives all of the 384 threads 168 registers; the first four warps hand 128 of theirs over to
+    // the other eight (40 + 2 * 232 = 3 * 168).
+    if (warp < 4) {
+        if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            if (lane == 0) {
+                int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
+                const int wstep = P.adjoint ? P.pfi : 1;
+                const CUtensorMap *amap = &P.a_map[r], *wmap = (P.adjoint ? &P.w_map[oblk] : &P.w_map[oblk * P.pfi]) + r * wstep;
+                const int nb0 = n0 + (int)prank * (TN / 2);
+                uint32_t s = 0, phase = 0, sa = base;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag)) break;
+                    const uint32_t full = bar_full + 8 * s, full_leader = map_to_cta(full, leader);
+                    if (prank == 0) mbar_expect_tx(full, 2 * C::kStageBytes);
+                    tma_load_2d_pair(sa, amap, kin * kF8K, m0, full_leader);                                              // box {128 k, 128 rows}
+                    if (!P.adjoint) tma_load_2d_pair(sa + C::kABytes, wmap, kin * kF8K, nb0, full_leader);                // box {128 k, TN / 2 rows}
+                    else tma_load_2d_pair(sa + C::kABytes, wmap, nb0, kin * kF8K, full_leader);                           // box {TN / 2 columns, 128 k}
+                    if (++kin == P.kpw) {
+                        kin = 0;
+                        ++amap;
+                        wmap += wstep;
+                    }
+                    sa += C::kStageBytes;
+                    if (++s == C::kStages) {
+                        s = 0;
+                        sa = base;
+                        phase ^= 1;
+                    }
+                }
+                if (*abort_flag) {
+                    // give copies that are still in flight time to land before the block retires
+                    const uint64_t t0 = global_timer();
+                    while (global_timer() - t0 < 1000000ull) {}
+                }
+            }
+            __syncwarp();
+        } else if (warp == 1) {
+            if (lane == 0 && prank == 0) {
+                const uint32_t idesc = f8_instr(2 * kF8Rows, TN, 0, P.adjoint);
+                // K-major: 8-row groups 1024 bytes apart, a K step of 32 values is 32 bytes.  MN-major: rows of TN / 2 columns (128-byte swizzle, or 64-byte
+                // where that is 64), 8-k groups 8 rows apart, a K step of 32 rows.
+                constexpr uint32_t row = TN / 2;
+                const uint64_t a0 = smem_desc(base, 16, 1024);
+                uint64_t b0 = smem_desc(base + C::kABytes, P.adjoint ? C::kBBytes : 16, P.adjoint ? 8 * row : 1024);
+                if (TN == 128 && P.adjoint) b0 = (b0 & ~((uint64_t)7 << 61)) | (uint64_t)4 << 61;
+                const uint64_t bstep = P.adjoint ? 32 * row >> 4 : 32 >> 4;
+                const uint16_t mask = (uint16_t)(3u << leader);
+                uint32_t s = 0, phase = 0;
+                uint64_t off = 0;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    const uint32_t it = (uint32_t)(kb - kb0), buf = it & 1u;
+                    if (!f8_wait(bar_free + 8 * buf, ((it >> 1) & 1u) ^ 1u, abort_flag)) break;
+                    if (!f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
+                    tcgen05_fence_after();
+                    const uint64_t a = a0 + off, b = b0 + off;
+                    const uint32_t d = tmem + buf * TN;
+                    umma_f8_pair(d, a, b, idesc, 0u);
+                    umma_f8_pair(d, a + 2, b + bstep, idesc, 1u);
+                    umma_f8_pair(d, a + 4, b + 2 * bstep, idesc, 1u);
+                    umma_f8_pair(d, a + 6, b + 3 * bstep, idesc, 1u);
+                    tcgen05_commit_mask(bar_empty + 8 * s, mask);
+                    tcgen05_commit_mask(bar_done + 8 * buf, mask);
+                    off += C::kStageBytes >> 4;
+                    if (++s == C::kStages) {
+                        s = 0;
+                        off = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        __syncwarp();
+        tcgen05_fence_before();
+        cluster_sync_all();
+        if (splits > 1) cluster_sync_all();
+        if (warp == 1) {
+            tcgen05_fence_after();
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * TN)) : "memory");
+        }
+    } else {
+        if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int quarter = warp & 3, half = (warp - 4) >> 2;               // tensor-memory lanes [32 q, 32 q + 32), columns [TN / 2 * half, ..)
+        const int row = m0 + quarter * 32 + lane, col = half * (TN / 2);
+        ScaleWalk walk(P, kb0, oblk, row, n0 + col);
+        uint64_t acc[TN / 4];
+#pragma unroll
+        for (int i = 0; i < TN / 4; ++i) acc[i] = 0ull;
+        constexpr int kAhead = 4;                                           // scales in flight
+        float next[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) next[i] = walk.next();
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col;
+        const uint32_t free_leader = map_to_cta(bar_free, leader);
+        bool ok = true;
+        for (int kb = kb0; ok && kb < kb1; kb += kAhead) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (kb + u >= kb1) break;
+                const uint32_t it = (uint32_t)(kb + u - kb0), buf = it & 1u;
+                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, (it >> 1) & 1u, abort_flag));
+                if (!ok) break;
+                tcgen05_fence_after();
+                const uint64_t s = pair_of(next[u], next[u]);
+                next[u] = walk.next();
+#pragma unroll
+                for (int c = 0; c < TN / 2; c += 32) {
+                    uint64_t d[16];
+                    tmem_ld32_pairs(taddr + buf * TN + c, d);
+                    if (c + 32 == TN / 2) {                                 // this half of tensor memory may be written again
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(free_leader + 8 * buf);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) fma_pair(acc[c / 2 + i], s, d[i]);
+                }
+            }
+        }
+        // every product has been taken, so the ring is free: the sums as [row][column]
+        if (ok) {
+            float *o = reinterpret_cast<float *>(aligned) + (quarter * 32 + lane) * C::kPitch + col;
+#pragma unroll
+            for (int i = 0; i < TN / 4; i += 2) {
+                const float2 lo = floats_of(acc[i]), hi = floats_of(acc[i + 1]);
+                *reinterpret_cast<float4 *>(o + 2 * i) = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+        }
+        tcgen05_fence_before();
+        cluster_sync_all();                                                 // every block's sums are in place
+        if (!*abort_flag) {
+            const int r0 = kF8Rows * split / splits, r1 = kF8Rows * (split + 1) / splits;
+            const float *bias = P.bias[oblk];
+#pragma unroll
+            for (int u = 0; u < TN / 128; ++u) {
+                const int c = 128 * u + 4 * lane, col = n0 + c;
+                if (col >= P.blk_out) continue;                                 // whole groups of four: blocks are multiples of 16
+                const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + col)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                for (int rl = r0 + warp - 4; rl < r1; rl += 8) {
+                    if (m0 + rl >= P.nb) break;
+                    const uint32_t addr = base + (uint32_t)((rl * C::kPitch + c) * 4);
+                    float4 v = ld_cluster_f4(map_to_cta(addr, prank));
+                    for (int q = 1; q < splits; ++q) {
+                        const float4 w = ld_cluster_f4(map_to_cta(addr, (uint32_t)(2 * q) + prank));
+                        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+                    }
+                    v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
+                    const int64_t at = (int64_t)(m0 + rl) * P.blk_out + col;
+                    if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[oblk]) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                    else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[oblk]) + at) = v;
+                }
+            }
+        }
+        if (splits > 1) cluster_sync_all();                                 // nobody retires while a peer reads its shared memory
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Few samples (a batch of at most 128): the weights are the M operand, 128 output features a block, the batch takes N = 16, 32, 64 or 128 columns.  A
+// cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds it is the stream of
+// the weights; two blocks an SM keep it going.
+// ------------------------------------------------------------------------------------------
+constexpr int kF8FewThreads = 192;                          // warp 0: TMA, warp 1: MMA and tensor memory, warps 2..5: sums
+constexpr int kF8WBytes = 128 * kF8K;
+constexpr int kF8FewMaxStages = 12;
+constexpr int kF8FewMaxSmem = 220 * 1024;                   // one block an SM; half of it: two
+
+struct AffineF8FewParams {
+    AffineF8Params p;
+    int32_t split, stages;
+};
+template <int N>
+struct F8FewCfg {
+    static constexpr int kStageBytes = kF8WBytes + N * kF8K;
+    static constexpr int kBuffers = N >= 128 ? 2 : N >= 64 ? 4 : 8;         // products in tensor memory
+    static constexpr int kTmemCols = kBuffers * N;
+    static constexpr int kMinStages = N >= 64 ? 3 : 2;                      // room for the sums: 512 N bytes
+    static constexpr int kScaleBytes = 4 * 2 * N * 4;                       // two sets of a k-block's scales for each of four warps
+    static constexpr int kTail = kF8Tail + kScaleBytes;
+    static_assert(kMinStages * kStageBytes >= 512 * N, "the sums take the ring's place");
+};
+
+template <int N>
+__global__ void __launch_bounds__(kF8FewThreads, 2)
+affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
+    stream_enter();
+    using C = F8FewCfg<N>;
+    const AffineF8Params &P = Q.p;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t *aligned = smem_raw + (base - raw);
+    float *scales = reinterpret_cast<float *>(aligned + Q.stages * C::kStageBytes);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + Q.stages * C::kStageBytes + C::kScaleBytes);
+    const uint32_t bar_full = smem_u32(bars);
+    const uint32_t bar_empty = bar_full + 8 * kF8FewMaxStages;
+    __shared__ __align__(8) uint64_t turn[2 * C::kBuffers];
+    const uint32_t bar_done = smem_u32(turn), bar_free = bar_done + 8 * C::kBuffers;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * kF8FewMaxStages);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_ctarank();
+    const int tile = (int)blockIdx.x / Q.split;
+    const int tiles_per_block = (P.blk_out + 127) / 128;
+    const int oblk = tile / tiles_per_block;
+    const int n0 = (tile - oblk * tiles_per_block) * 128;   // first output feature inside the block
+    const int all = P.nred * P.kpw;
+    const int kb0 = (int)((int64_t)all * rank / Q.split), kb1 = (int)((int64_t)all * (rank + 1) / Q.split);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < Q.stages; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int b = 0; b < C::kBuffers; ++b) {
+            mbar_init(bar_done + 8 * b, 1);
+            mbar_init(bar_free + 8 * b, 4);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)C::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
+            const int wstep = P.adjoint ? P.pfi : 1;
+            const CUtensorMap *wmap = (P.adjoint ? &P.w_map[oblk] : &P.w_map[oblk * P.pfi]) + r * wstep;
+            uint32_t s = 0, phase = 0, sa = base;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag)) break;
+                const uint32_t full = bar_full + 8 * s;
+                mbar_expect_tx(full, C::kStageBytes);
+                if (!P.adjoint) tma_load_2d(sa, wmap, kin * kF8K, n0, full);               // K-major: box {128 k, 128 features}
+                else tma_load_2d(sa, wmap, n0, kin * kF8K, full);                          // MN-major: box {128 features, 128 k}
+                tma_load_2d(sa + kF8WBytes, &P.a_map[r], kin * kF8K, 0, full);             // box {128 k, N rows}
+                if (++kin == P.kpw) {
+                    kin = 0;
+                    ++r;
+                    wmap += wstep;
+                }
+                sa += C::kStageBytes;
+                if (++s == (uint32_t)Q.stages) {
+                    s = 0;
+                    sa = base;
+                    phase ^= 1;
+                }
+            }
+            if (*abort_flag) {
+                const uint64_t t0 = global_timer();
+                while (global_timer() - t0 < 1000000ull) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = f8_instr(128, N, P.adjoint, 0);
+            const uint64_t a0 = smem_desc(base, P.adjoint ? kF8WBytes : 16, 1024);
+            const uint64_t astep = P.adjoint ? 32 * 128 >> 4 : 32 >> 4;
+            const uint64_t b0 = smem_desc(base + kF8WBytes, 16, 1024);
+            uint32_t s = 0, phase = 0, buf = 0, bphase = 0;
+            uint64_t off = 0;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!f8_wait(bar_free + 8 * buf, bphase ^ 1, abort_flag)) break;
+                if (!f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
+                tcgen05_fence_after();
+                const uint64_t a = a0 + off, b = b0 + off;
+                const uint32_t d = tmem + buf * N;
+                umma_f8(d, a, b, idesc, 0u);
+                umma_f8(d, a + astep, b + 2, idesc, 1u);
+                umma_f8(d, a + 2 * astep, b + 4, idesc, 1u);
+                umma_f8(d, a + 3 * astep, b + 6, idesc, 1u);
+                tcgen05_commit(bar_empty + 8 * s);
+                tcgen05_commit(bar_done + 8 * buf);
+                off += C::kStageBytes >> 4;
+                if (++s == (uint32_t)Q.stages) {
+                    s = 0;
+                    off = 0;
+                    phase ^= 1;
+                }
+                if (++buf == C::kBuffers) {
+                    buf = 0;
+                    bphase ^= 1;
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // A lane is a feature; the samples' scales, times the weights' one, go through shared memory of the warp's own, two sets in turn.
+        const int quarter = warp & 3;
+        constexpr int kPer = (N + 31) / 32, kAhead = N >= 128 ? 2 : 4;
+        float *mine = scales + quarter * 2 * N;
+        int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
+        const auto fetch = [&](float *s) {                                  // the next k-block's scales, those of `lane`, `lane` + 32, ...
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) s[i] = 0.f;
+            if (r >= P.nred) return;
+            const float w = __ldg(P.ws[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r] + (int64_t)kin * P.ws_k + (int64_t)(n0 / kScaleBlock) * P.ws_n);
+            const float *a = P.as[r] + (int64_t)kin * P.nb;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (lane + 32 * i < P.nb) s[i] = __ldg(a + lane + 32 * i) * w;
+            if (++kin == P.kpw) {
+                kin = 0;
+                ++r;
+            }
+        };
+        float next[kAhead][kPer];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(next[i]);
+        uint64_t acc[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) acc[i] = 0ull;
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
+        uint32_t buf = 0, bphase = 0;
+        bool ok = true;
+        for (int kb = kb0; ok && kb < kb1; kb += kAhead) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (kb + u >= kb1) break;
+                float *set = mine + (u & 1) * N;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (N % 32 == 0 || lane + 32 * i < N) set[lane + 32 * i] = next[u][i];
+                fetch(next[u]);
+                __syncwarp();
+                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, bphase, abort_flag));
+                if (!ok) break;
+                tcgen05_fence_after();
+#pragma unroll
+                for (int c = 0; c < N; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(taddr + buf * N + c, v);
+                    if (c + 16 == N) {
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar_free + 8 * buf);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 s = *reinterpret_cast<const float4 *>(set + c + i);
+                        fma_pair(acc[(c + i) / 2], pair_of(s.x, s.y), (uint64_t)v[i] | (uint64_t)v[i + 1] << 32);
+                        fma_pair(acc[(c + i) / 2 + 1], pair_of(s.z, s.w), (uint64_t)v[i + 2] | (uint64_t)v[i + 3] << 32);
+                    }
+                }
+                if (++buf == C::kBuffers) {
+                    buf = 0;
+                    bphase ^= 1;
+                }
+            }
+        }
+        // the blocks' other warps have no use for the ring once every product has been taken: the sums as [sample][feature]
+        if (ok) {
+            float *part = reinterpret_cast<float *>(aligned) + quarter * 32 + lane;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float2 f = floats_of(acc[i]);
+                part[(2 * i) * 128] = f.x;
+                part[(2 * i + 1) * 128] = f.y;
+            }
+        }
+    }
+    tcgen05_fence_before();
+    cluster_sync_all();                                     // every block's sums are in place
+    if (!*abort_flag) {
+        const int rows = (P.nb + Q.split - 1) / Q.split, row0 = rank * rows, row1 = min(P.nb, row0 + rows);
+        const int f = 4 * lane;
+        if (n0 + f < P.blk_out) {
+            const float4 bias = P.bias[oblk] ? __ldg(reinterpret_cast<const float4 *>(P.bias[oblk] + n0 + f)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int row = row0 + warp; row < row1; row += kF8FewThreads / 32) {
+                const uint32_t addr = base + (uint32_t)((row * 128 + f) * 4);
+                float4 o = ld_cluster_f4(map_to_cta(addr, 0));
+                for (int q = 1; q < Q.split; ++q) {
+                    const float4 v = ld_cluster_f4(map_to_cta(addr, (uint32_t)q));
+                    o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+                }
+                o.x += bias.x, o.y += bias.y, o.z += bias.z, o.w += bias.w;
+                const int64_t at = (int64_t)row * P.blk_out + n0 + f;
+                if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[oblk]) + at) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+                else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[oblk]) + at) = o;
+            }
+        }
+    }
+    cluster_sync_all();                                     // nobody retires while a peer reads its shared memory
+    if (warp == 1) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::kTmemCols) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------
+// Row-major matrix of bytes [rows, cols]; box = {box_cols (inner, 128 or 64), box_rows}, swizzled by its inner extent.
+static bool make_map_u8(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, int box_cols, int box_rows) {
+    EncodeTiledFn fn = tensor_map_encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)cols};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              box_cols == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int N>
+static distdl_status_t launch_few(const AffineF8Params &P, int64_t tiles, int sms, cudaStream_t stream) {
+    // blocks of a tile: doubled while twice as many blocks as SMs are not exceeded and every block keeps four k-blocks
+    AffineF8FewParams Q;
+    Q.p = P;
+    Q.split = 1;
+    const int64_t all = (int64_t)P.nred * P.kpw;
+    while (Q.split < 8 && tiles * Q.split * 2 <= 2 * sms && all >= 4 * 2 * Q.split) Q.split *= 2;
+    const int budget = tiles * Q.split <= sms ? kF8FewMaxSmem : kF8FewMaxSmem / 2;
+    Q.stages = std::min(kF8FewMaxStages, (budget - F8FewCfg<N>::kTail) / F8FewCfg<N>::kStageBytes);
+    const int smem = Q.stages * F8FewCfg<N>::kStageBytes + F8FewCfg<N>::kTail;
+    launch_clusters_in_stream(affine_fp8_few_kernel<N>, (unsigned)Q.split, dim3((unsigned)(tiles * Q.split)), dim3(kF8FewThreads), (size_t)smem, stream, Q);
+    return DISTDL_OK;
+}
+
+static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *act, const void *const *act_scales,
+                                       const void *const *w, const void *const *ws, const void *const *bias, distdl_dtype_t t, void *const *out, void *stream,
+                                       bool adjoint, const char *what) {
+    clear_error();
+    if (nb < 1 || nfi < 1 || nfo < 1 || pfo < 1 || pfi < 1) return fail(DISTDL_ERR_INVALID_ARG, "%s: non-positive size", what);
+    if (t != DISTDL_F32 && t != DISTDL_BF16) return fail(DISTDL_ERR_INVALID_ARG, "%s: results are F32 or BF16", what);
+    if (nfi % pfi || nfo % pfo) return fail(DISTDL_ERR_SHAPE, "%s: features not divisible by the worker grid", what);
+    const int64_t bfi = nfi / pfi, bfo = nfo / pfo;
+    if (bfi % 16 || bfo % 16)
+        return fail(DISTDL_ERR_UNSUPPORTED, "%s: per-worker feature blocks must be multiples of 16 (rows of whole 16-byte units)", what);
+    if (pfo > 8 || pfi > 8 || pfo * pfi > kF8MaxWorkers)
+        return fail(DISTDL_ERR_UNSUPPORTED, "%s: worker grid larger than 8 per side or %d workers", what, kF8MaxWorkers);
+    if (nb > (1 << 20) || bfi > (1 << 22) || bfo > (1 << 22)) return fail(DISTDL_ERR_UNSUPPORTED, "%s: more than 2^20 samples or 2^22 features a worker", what);
+    const int nact = adjoint ? pfo : pfi, nout = adjoint ? pfi : pfo, grid = pfo * pfi;
+    distdl_status_t st;
+    if ((st = check_blocks(what, adjoint ? "dy" : "x", act, nact)) || (st = check_blocks(what, adjoint ? "dys" : "xs", act_scales, nact)) ||
+        (st = check_blocks(what, "w", w, grid)) || (st = check_blocks(what, "ws", ws, grid)) || (st = check_blocks(what, adjoint ? "dx" : "y", out, nout)))
+        return st;
+    for (int i = 0; bias && i < nout; ++i)
+        if (bias[i] && !aligned16(bias[i])) return fail(DISTDL_ERR_ALIGNMENT, "%s: bias[%d] not 16-byte aligned", what, i);
+    int device, sms;
+    if ((st = current_device(what, act[0], &device)) || (st = multiprocessors(device, &sms))) return st;
+    if (!tensor_map_encoder()) return fail(DISTDL_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available", what);
+
+    AffineF8Params P;
+    memset(&P, 0, sizeof(P));
+    P.nb = (int32_t)nb;
+    P.pfi = pfi;
+    P.blk_out = (int32_t)(adjoint ? bfi : bfo);
+    P.blk_red = (int32_t)(adjoint ? bfo : bfi);
+    P.nred = nact;
+    P.kpw = (int32_t)scale_blocks(P.blk_red);
+    const int32_t scale_cols = (int32_t)scale_blocks(bfi);
+    P.ws_k = adjoint ? scale_cols : 1;
+    P.ws_n = adjoint ? 1 : scale_cols;
+    P.adjoint = adjoint ? 1 : 0;
+    P.out_bf16 = t == DISTDL_BF16;
+    for (int i = 0; i < nact; ++i) P.as[i] = (const float *)act_scales[i];
+    for (int i = 0; i < grid; ++i) P.ws[i] = (const float *)ws[i];
+    for (int i = 0; i < nout; ++i) {
+        P.out[i] = out[i];
+        P.bias[i] = bias ? (const float *)bias[i] : nullptr;
+    }
+
+    static bool configured_on[kMaxDevicesPerProcess] = {false};
+    {
+        std::lock_guard<std::mutex> setup_lock(setup_mutex());
+        if (!configured_on[device]) {
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+            configured_on[device] = true;
+        }
+    }
+    const bool few = nb <= kF8Rows;
+    const int n = nb <= 16 ? 16 : nb <= 32 ? 32 : nb <= 64 ? 64 : 128;
+    // tile width and splits of the contraction: fewest clocks by a count of turns (see the measured clocks of a k-block below)
+    int tn = 256, splits = 1;
+    const int64_t row_tiles = (nb + 2 * kF8Rows - 1) / (2 * kF8Rows), all = (int64_t)P.nred * P.kpw;
+    if (!few) {
+        double best = 0;
+        for (int width : {256, 128})
+            for (int s : {1, 2, 4}) {
+                if (s > 1 && all < 8 * s) continue;
+                const int64_t tiles = row_tiles * nout * ((P.blk_out + width - 1) / width);
+                const int64_t at_once = std::max(1, sms / (2 * s)), turns = (tiles + at_once - 1) / at_once;
+                const double clocks = (double)turns * ((double)((all + s - 1) / s) * (width == 256 ? 600 : 400) + (width == 256 ? 5000 : 3500) + (s > 1 ? 1000 * s : 0));
+                if (best == 0 || clocks < best) {
+                    best = clocks;
+                    tn = width;
+                    splits = s;
+                }
+            }
+    }
+    for (int i = 0; i < nact; ++i)
+        if (!make_map_u8(&P.a_map[i], act[i], nb, P.blk_red, kF8K, few ? n : kF8Rows))
+            return fail(DISTDL_ERR_CUDA, "%s: tensor map of activation block %d failed", what, i);
+    for (int i = 0; i < grid; ++i) {
+        // weights: the columns of a tile that a block stages, by 128 of the contraction
+        const int columns = few ? 128 : tn / 2;
+        const bool ok = adjoint ? make_map_u8(&P.w_map[i], w[i], bfo, bfi, columns, kF8K) : make_map_u8(&P.w_map[i], w[i], bfo, bfi, kF8K, columns);
+        if (!ok) return fail(DISTDL_ERR_CUDA, "%s: tensor map of weight block %d failed", what, i);
+    }
+    const cudaStream_t in = (cudaStream_t)stream;
+    if (few) {
+        const int64_t tiles = nout * scale_blocks(P.blk_out);
+        if (n == 16) launch_few<16>(P, tiles, sms, in);
+        else if (n == 32) launch_few<32>(P, tiles, sms, in);
+        else if (n == 64) launch_few<64>(P, tiles, sms, in);
+        else launch_few<128>(P, tiles, sms, in);
+    } else {
+        const int64_t blocks = row_tiles * nout * ((P.blk_out + tn - 1) / tn) * 2 * splits;
+        if (blocks > INT32_MAX) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
+        if (tn == 256) launch_clusters_in_stream(affine_fp8_pair_kernel<256>, 2u * splits, dim3((unsigned)blocks), dim3(kF8Threads), F8Cfg<256>::kSmemBytes, in, P);
+        else launch_clusters_in_stream(affine_fp8_pair_kernel<128>, 2u * splits, dim3((unsigned)blocks), dim3(kF8Threads), F8Cfg<128>::kSmemBytes, in, P);
+    }
+    DISTDL_CUDA_CHECK(cudaGetLastError());
+    return DISTDL_OK;
+}
+
+}  // namespace distdl
+
+extern "C" distdl_status_t distdl_affine_fp8_fwd(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *x,
+                                                 const void *const *xs, const void *const *w, const void *const *ws, const void *const *bias,
+                                                 distdl_dtype_t t, void *const *y, void *stream) {
+    return distdl::affine_fp8_impl(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, t, y, stream, false, "affine_fp8_fwd");
+}
+
+extern "C" distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *dy,
+                                                 const void *const *dys, const void *const *w, const void *const *ws, distdl_dtype_t t, void *const *dx,
+                                                 void *stream) {
+    return distdl::affine_fp8_impl(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, nullptr, t, dx, stream, true, "affine_fp8_adj");
+}

@@ -235,6 +235,7 @@ PyMethodDef methods[] = {
     FUNCTION(stencil3d_fwd), FUNCTION(stencil3d_adj), FUNCTION(pool_fwd), FUNCTION(pool_adj),
     FUNCTION(affine_fwd), FUNCTION(affine_adj), FUNCTION(affine_adj_params),
     FUNCTION(quantize_rows), FUNCTION(quantize_weights), FUNCTION(rmsnorm_fwd), FUNCTION(rmsnorm_adj), FUNCTION(adamw_step),
+    FUNCTION(affine_fp8_fwd), FUNCTION(affine_fp8_adj),
     {"taps", taps, METH_O, nullptr},
     {"set_stream_lookup", (PyCFunction)(void (*)(void))set_stream_lookup, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -469,3 +469,74 @@ def test_adamw_beyond_32_bits_of_elements():
         want, sw = o.moment_to_8_bits(value, u / 65536.0, positive)
         assert (f64(code[at:]) != want).mean() <= 3e-3 and np.allclose(f64(scale[at // 128:]), sw, rtol=12 * U)
     assert not p[:at].any() and not m.view(torch.uint8)[:at].any() and p[at:].ne(dev(pw)).any()
+
+
+# ---------------------------------------------------------------------------------------------
+# The affine layer in 8 bits
+# ---------------------------------------------------------------------------------------------
+
+# nb, features of a worker's input and output block, grid
+FP8 = [(1, 16, 16, 1, 1), (1, 128, 128, 1, 1), (2, 144, 272, 2, 3), (16, 2048, 2048, 2, 2), (17, 400, 112, 1, 2), (33, 1040, 656, 2, 2), (64, 256, 128, 4, 1),
+       (65, 48, 1040, 1, 4), (100, 128, 2048, 1, 1), (128, 1296, 32, 3, 2), (129, 128, 128, 1, 1), (129, 16, 16, 2, 2), (200, 272, 656, 2, 3), (256, 2048, 256, 1, 2),
+       (256, 512, 1024, 2, 4), (300, 144, 144, 1, 1), (513, 1040, 80, 3, 1), (777, 208, 400, 2, 2), (1500, 640, 1280, 1, 1), (3000, 256, 2048, 1, 1), (1000, 4096, 96, 1, 4)]
+
+
+def fp8_inputs(nb, bfi, bfo, pfo, pfi, adj, exact, seed=600):
+    """Activations, weights as (values, scales) pairs.  exact: whole numbers, scales that are powers of two, sums below 2^24 steps."""
+    blk, n = (bfo, pfo) if adj else (bfi, pfi)
+    if exact:
+        pow2 = lambda shape, s: np.float32(2.0) ** inputs.integers(shape, s, 0, 3)  # noqa: E731
+        a = [(inputs.integers((nb, blk), seed + j, -2, 3).astype(np.float64), pow2((-(-blk // 128), nb), seed + 50 + j)) for j in range(n)]
+        w = [(inputs.integers((bfo, bfi), seed + 100 + i, -2, 3).astype(np.float64), pow2((-(-bfo // 128), -(-bfi // 128)), seed + 150 + i)) for i in range(pfo * pfi)]
+    else:
+        a = [o.quantize_rows(inputs.normal((nb, blk), seed + j) * np.float32(3.0) ** inputs.integers((nb, 1), seed + 50 + j, -3, 4)) for j in range(n)]
+        w = [o.quantize_weights(inputs.normal((bfo, bfi), seed + 100 + i, 0.05)) for i in range(pfo * pfi)]
+    return a, w
+
+
+def fp8_call(nb, bfi, bfo, pfo, pfi, adj, a, w, bias, t, out):
+    ad, asd = [dev(v, E4) for v, _ in a], [dev(s) for _, s in a]
+    wd, wsd = [dev(v, E4) for v, _ in w], [dev(s) for _, s in w]
+    y = [out(nb, bfi if adj else bfo, dtype=t) for _ in range(pfi if adj else pfo)]
+    if adj:
+        distdl.affine_fp8_adj(nb, bfi * pfi, bfo * pfo, pfo, pfi, ad, asd, wd, wsd, y)
+    else:
+        distdl.affine_fp8_fwd(nb, bfi * pfi, bfo * pfo, pfo, pfi, ad, asd, wd, wsd, None if bias is None else [dev(b) for b in bias], y)
+    distdl.device_status()
+    return y
+
+
+@pytest.mark.parametrize("adj", [False, True], ids=["fwd", "adj"])
+@pytest.mark.parametrize("case", FP8, ids=str)
+def test_affine_fp8_on_whole_numbers(case, adj):
+    """Every product and sum is exact in fp32 (at most 2^16 of them, each at most 64 steps): equal to the oracle in any order."""
+    nb, bfi, bfo, pfo, pfi = case
+    a, w = fp8_inputs(*case, adj, True)
+    bias = None if adj else [inputs.integers((bfo,), 700 + i) for i in range(pfo)]
+    want = o.affine_fp8_adj(a, w, pfo, pfi) if adj else o.affine_fp8_fwd(a, w, pfo, pfi, bias)
+    for t in (torch.float32, torch.bfloat16):
+        out = Out()
+        for got, ref in zip(fp8_call(*case, adj, a, w, bias, t, out), want):
+            assert np.array_equal(f64(got), rounded(ref.astype(np.float32), t).astype(np.float64))
+        out.check()
+
+
+@pytest.mark.parametrize("adj", [False, True], ids=["fwd", "adj"])
+@pytest.mark.parametrize("case", FP8, ids=str)
+def test_affine_fp8_on_normal_numbers(case, adj):
+    nb, bfi, bfo, pfo, pfi = case
+    a, w = fp8_inputs(*case, adj, False)
+    bias = None if adj else [inputs.normal((bfo,), 700 + i) for i in range(pfo)]
+    fn = o.affine_fp8_adj if adj else o.affine_fp8_fwd
+    want = fn(a, w, pfo, pfi) if adj else fn(a, w, pfo, pfi, bias)
+    size = fn([(np.abs(v), s) for v, s in a], [(np.abs(v), s) for v, s in w], pfo, pfi)
+    # 128 additions of a product in the tensor cores, where a sum may be cut off instead of rounded (2 U each), the scales' product, a rounding per block
+    blocks = -(-(bfo if adj else bfi) // 128) * (pfo if adj else pfi)
+    for t in (torch.float32, torch.bfloat16):
+        out = Out()
+        for j, (got, ref, s) in enumerate(zip(fp8_call(*case, adj, a, w, bias, t, out), want, size)):
+            e = (2 * 128 + 2 + blocks + 8) * U * (s + (0 if bias is None else np.abs(bias[j])))
+            assert (np.abs(f64(got) - ref) <= e + eps_of(t) * (np.abs(ref) + e)).all()
+            if t is torch.float32:
+                assert np.linalg.norm(f64(got) - ref) <= 1e-6 * np.linalg.norm(s)
+        out.check()

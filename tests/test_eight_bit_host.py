@@ -231,3 +231,37 @@ def test_adamw_handle_refuses_tensors_that_do_not_belong_together():
         opt.step(f(), 1e-3, 0, stream=0)
     assert e.value.status == 1
     distdl.AdamW([], [], []).step([], 1e-3, 1)
+
+
+def test_affine_fp8_refusals():
+    lib, a, odd = distdl.lib(), _array(16), _array(16, first=0x10008)
+
+    def fwd(nb=16, nfi=256, nfo=256, pfo=1, pfi=1, x=a, xs=a, w=a, ws=a, bias=a, t=distdl.F32, y=a):
+        return lib.distdl_affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, t, y, None)
+
+    def adj(nb=16, nfi=256, nfo=256, pfo=1, pfi=1, x=a, xs=a, w=a, ws=a, t=distdl.BF16, y=a):
+        return lib.distdl_affine_fp8_adj(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, t, y, None)
+
+    for call in (fwd, adj):
+        assert call(nb=0) == 1 and call(nfi=0) == 1 and call(pfo=0) == 1 and call(nfi=256, pfi=3) == 2 and call(nfo=100, pfo=3) == 2
+        assert call(nfi=264) == 4 and call(nfo=8) == 4 and call(pfo=16) == 4 and call(pfo=4, pfi=8) == 4 and call(nb=(1 << 20) + 1) == 4
+        assert call(t=distdl.F64) == 1 and call(t=distdl.E4M3) == 1
+        for name in ("x", "xs", "w", "ws", "y"):
+            assert call(**{name: None}) == 1 and call(**{name: odd}) == 3 and call(**{name: (vp * 1)(None)}) == 1, name
+    assert fwd(bias=odd) == 3
+    e4, t = torch.float8_e4m3fn, lambda *shape, dtype=torch.float32: torch.zeros(*shape, dtype=dtype)
+    x, xs, w, ws, y = [t(4, 128, dtype=e4)] * 2, [t(1, 4)] * 2, [t(144, 128, dtype=e4)] * 2, [t(2, 1)] * 2, [t(4, 144)]
+
+    def refused(status, *args):
+        with pytest.raises(distdl.DistdlError) as e:
+            distdl.affine_fp8_fwd(4, 256, 144, 1, 2, *args, stream=0)
+        assert e.value.status == status
+
+    refused(1, x[:1], xs, w, ws, None, y)
+    refused(1, x, xs[:1], w, ws, None, y)
+    refused(1, x, xs, w[:1], ws, None, y)
+    refused(1, x, xs, w, ws, [], y)
+    refused(2, x, xs, w, [t(1, 1)] * 2, None, y)
+    refused(2, x, xs, [t(128, 144, dtype=e4).t()] * 2, ws, None, y)
+    refused(2, x, [t(4)[:0]] * 2, w, ws, None, y)
+    refused(2, x, xs, w, ws, [t(143)], y)
