@@ -22,7 +22,6 @@ namespace distdl {
 
 constexpr int kF8K = 128;                                   // of the contraction at a time: one scale, one 128-byte swizzle row
 constexpr int kF8Rows = 128;                                // rows of a thread block's tile
-constexpr int kF8Threads = 384;                             // warp 0: TMA, warp 1: MMA and tensor memory, warps 4..11: sums
 constexpr int kF8MaxWorkers = 16;
 
 __device__ int g_fp8_status = 0;                            // 0 or DISTDL_ERR_TIMEOUT
@@ -48,7 +47,8 @@ struct AffineF8Params {
     int32_t nred;                                           // workers summed over
     int32_t kpw;                                            // k-blocks of a worker
     int32_t ws_k, ws_n;                                     // steps in the weights' scales: to the next k-block, the next 128 columns
-    int32_t adjoint, out_bf16;
+    int32_t nout, tiles, splits;                            // output blocks; tiles and splits of the contraction (pairs)
+    int32_t adjoint, out_bf16, out_wide;                    // out_wide: every output block begins on a 32-byte boundary
 };
 
 __device__ __forceinline__ bool f8_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
@@ -74,12 +74,14 @@ __device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t adesc, ui
 __host__ __device__ constexpr uint32_t f8_instr(int m, int n, int a_mn, int b_mn) {
     return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+// Arrival at a barrier of another block of the cluster.  What it releases is tensor memory (the fence before it sees to that), so it takes no fence at the
+// cluster's scope: that one, once a k-block for each warp, was the largest stall of the kernel.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
 // acc += s * d for pairs of floats
 __device__ __forceinline__ void fma_pair(uint64_t &acc, uint64_t s, uint64_t d) {
-    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(s), "l"(d));
+    asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(s), "l"(d));
 }
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
     uint64_t r;
@@ -91,64 +93,87 @@ __device__ __forceinline__ float2 floats_of(uint64_t v) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
     return f;
 }
-// 32 columns of tensor memory, in pairs
-__device__ __forceinline__ void tmem_ld32_pairs(uint32_t taddr, uint64_t *d) {
-    uint32_t v[32];
-    tmem_ld32(taddr, v);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) d[i] = (uint64_t)v[2 * i] | (uint64_t)v[2 * i + 1] << 32;
+// 4 bytes, or four zeros, to shared memory, and an arrival at a barrier once this thread's copies so far are there.
+__device__ __forceinline__ void copy_float_async(uint32_t dst, const float *src, bool there) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4u : 0u) : "memory");
 }
-
-// Walks through the scales of one row of the activations and one block of columns of the weights, k-block by k-block, worker by worker.
-struct ScaleWalk {
-    const AffineF8Params &P;
-    int r, kin, oblk, row, nblk;
-    const float *a, *w;
-    bool row_there, col_there;
-    __device__ __forceinline__ ScaleWalk(const AffineF8Params &p, int kb, int oblk_, int row_, int col)
-        : P(p), r(kb / p.kpw), kin(kb - kb / p.kpw * p.kpw), oblk(oblk_), row(row_), nblk(col / kScaleBlock), row_there(row_ < p.nb), col_there(col < p.blk_out) {
-        seek();
-    }
-    __device__ __forceinline__ void seek() {
-        if (r < P.nred) {
-            a = P.as[r] + (int64_t)kin * P.nb + row;
-            w = P.ws[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r] + (int64_t)kin * P.ws_k + (int64_t)nblk * P.ws_n;
-        }
-    }
-    __device__ __forceinline__ float next() {
-        float s = 0.f;
-        if (r < P.nred && row_there && col_there) s = __ldg(a) * __ldg(w);
-        a += P.nb;
-        w += P.ws_k;
-        if (++kin == P.kpw) {
-            kin = 0;
-            ++r;
-            seek();
-        }
-        return s;
-    }
-};
+__device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
 
 // ------------------------------------------------------------------------------------------
 // Batches over 128: a pair of blocks owns a 256 x TN tile (cta_group::2, 128 rows and half of the weights' columns each); a cluster of S pairs shares the
 // k-blocks of a tile, in S runs one after the other, and adds up the S sums through distributed shared memory in that order.
 // ------------------------------------------------------------------------------------------
-constexpr int kF8Tail = 1024 + 256;                         // alignment, barriers
+constexpr int kF8Tail = 1024 + 512;                         // alignment, barriers
+constexpr int kF8ScaleSlots = 8;                            // k-blocks whose scales are on their way or waited for
+constexpr int kF8ScaleSlot = kF8Rows + 8;                   // floats: the rows' scales, the two column halves' weight scales
 template <int TN>
 struct F8Cfg {
+    static constexpr int kSumWarps = TN / 64 * 4;           // 64 columns of 32 rows each
+    static constexpr int kThreads = 128 + 32 * kSumWarps;   // warp 0: TMA, warp 1: MMA and tensor memory, warp 2: scales, warps 4..: sums
     static constexpr int kABytes = kF8Rows * kF8K;          // 16 KB
     static constexpr int kBBytes = TN / 2 * kF8K;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = 196608 / kStageBytes;    // 6 or 8
     static constexpr int kPitch = TN + 4;                   // floats of a row of sums in shared memory; spreads rows over the banks
-    static constexpr int kSmemBytes = kStages * kStageBytes + kF8Tail;
+    static constexpr int kScaleBytes = kF8ScaleSlots * kF8ScaleSlot * 4;
+    static constexpr int kSmemBytes = kStages * kStageBytes + kScaleBytes + kF8Tail;
     static_assert(kF8Rows * kPitch * 4 <= kStages * kStageBytes, "the sums take the ring's place");
-    static_assert((2 * kStages + 4) * 8 + 8 <= 256, "barriers");
-    static_assert(kStages >= 2, "");
+    static_assert(TN % kScaleBlock == 0, "");
+    static constexpr int kBars = 2 * kStages + 4 + 2 * kF8ScaleSlots;
+    static_assert(kBars * 8 + 8 <= 512, "barriers");
 };
 
-template <int TN>
-__global__ void __launch_bounds__(kF8Threads, 1)
+// Tiles in groups of eight rows of tiles, column by column inside a group, so that what runs at a time shares its rows and columns in L2.
+constexpr int kF8GroupRows = 8;
+struct F8Tile {
+    int m0, n0, oblk;                                       // first row of the tile, first column inside the output block
+    template <int TN>
+    static __device__ __forceinline__ F8Tile of(const AffineF8Params &P, int tile) {
+        const int row_tiles = (P.nb + 2 * kF8Rows - 1) / (2 * kF8Rows), per_block = (P.blk_out + TN - 1) / TN, columns = P.nout * per_block;
+        const int group = tile / (kF8GroupRows * columns), first = group * kF8GroupRows, rows = min(kF8GroupRows, row_tiles - first);
+        const int in = tile - first * columns, column = in / rows;
+        F8Tile t;
+        t.m0 = (first + in - column * rows) * 2 * kF8Rows;
+        t.oblk = column / per_block;
+        t.n0 = (column - t.oblk * per_block) * TN;
+        return t;
+    }
+};
+
+// 16 values of a row: two 16-byte stores, or one of 32 bytes where the buffer allows it.
+__device__ __forceinline__ void f8_store(const AffineF8Params &P, int oblk, int64_t at, const float *v) {
+    if (P.out_bf16) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        uint16_t *p = reinterpret_cast<uint16_t *>(P.out[oblk]) + at;
+        if (P.out_wide) {
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        } else {
+            st_bytes<16>(p, w);
+            st_bytes<16>(p + 8, w + 4);
+        }
+    } else {
+        float *p = reinterpret_cast<float *>(P.out[oblk]) + at;
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            if (P.out_wide) {
+                asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]), "f"(v[i + 4]), "f"(v[i + 5]),
+                             "f"(v[i + 6]), "f"(v[i + 7]) : "memory");
+            } else {
+                *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                *reinterpret_cast<float4 *>(p + i + 4) = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
+            }
+        }
+    }
+}
+
+// SPLIT: a cluster of S pairs takes one tile.  Otherwise a pair goes from tile to tile, and copies and products of the next one begin while the
+// sums of the last one are written.
+template <int TN, bool SPLIT>
+__global__ void __launch_bounds__(F8Cfg<TN>::kThreads, 1)
 affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     stream_enter();
     using C = F8Cfg<TN>;
@@ -156,25 +181,21 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;           // the swizzle is a function of address bits [7,10)
     uint8_t *aligned = smem_raw + (base - raw);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + C::kStages * C::kStageBytes);
+    const float *scales = reinterpret_cast<const float *>(aligned + C::kStages * C::kStageBytes);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + C::kStages * C::kStageBytes + C::kScaleBytes);
     const uint32_t bar_full = smem_u32(bars);
     const uint32_t bar_empty = bar_full + 8 * C::kStages;
     const uint32_t bar_done = bar_empty + 8 * C::kStages;   // two: a product of 128 is in tensor memory
     const uint32_t bar_free = bar_done + 16;                // two: it has been taken
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * C::kStages + 4);
+    const uint32_t bar_scale = bar_free + 16;               // a k-block's scales are in shared memory
+    const uint32_t bar_scale_free = bar_scale + 8 * kF8ScaleSlots;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t crank = cluster_ctarank(), prank = crank & 1, leader = crank & ~1u;
-    uint32_t cluster_size;
-    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(cluster_size));
-    const int splits = (int)cluster_size / 2, split = (int)crank / 2;
-    const int tile = (int)(blockIdx.x / cluster_size);
-    const int row_tiles = (P.nb + 2 * kF8Rows - 1) / (2 * kF8Rows);
-    const int m0 = (tile % row_tiles) * 2 * kF8Rows + (int)prank * kF8Rows;
-    const int tiles_per_block = (P.blk_out + TN - 1) / TN;
-    const int oblk = tile / row_tiles / tiles_per_block;
-    const int n0 = (tile / row_tiles - oblk * tiles_per_block) * TN;
+    const int splits = SPLIT ? P.splits : 1, split = SPLIT ? (int)crank / 2 : 0;
+    const int first_tile = (int)blockIdx.x / (2 * splits), tile_step = (int)gridDim.x / (2 * splits);
     const int all = P.nred * P.kpw;
     const int kb0 = (int)((int64_t)all * split / splits), kb1 = (int)((int64_t)all * (split + 1) / splits);
 
@@ -185,7 +206,11 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_done + 8 * b, 1);
-            mbar_init(bar_free + 8 * b, 16);                // the summing warps of both blocks
+            mbar_init(bar_free + 8 * b, 2 * C::kSumWarps);  // the summing warps of both blocks
+        }
+        for (int s = 0; s < kF8ScaleSlots; ++s) {
+            mbar_init(bar_scale + 8 * s, 32);               // the lanes that copy
+            mbar_init(bar_scale_free + 8 * s, C::kSumWarps); // the summing warps
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -199,34 +224,35 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // 256 columns: a summing thread holds 128 sums.  The launch gives all of the 384 threads 168 registers; the first four warps hand 128 of theirs over to
-    // the other eight (40 + 2 * 232 = 3 * 168).
+    // 256 columns: the launch gives all of the 640 threads 96 registers; the first four warps hand 64 of theirs over to the sixteen that hold the sums
+    // (32 + 4 * 112 = 5 * 96).
     if (warp < 4) {
-        if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
         if (warp == 0) {
             if (lane == 0) {
-                int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
-                const int wstep = P.adjoint ? P.pfi : 1;
-                const CUtensorMap *amap = &P.a_map[r], *wmap = (P.adjoint ? &P.w_map[oblk] : &P.w_map[oblk * P.pfi]) + r * wstep;
-                const int nb0 = n0 + (int)prank * (TN / 2);
-                uint32_t s = 0, phase = 0, sa = base;
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag)) break;
-                    const uint32_t full = bar_full + 8 * s, full_leader = map_to_cta(full, leader);
-                    if (prank == 0) mbar_expect_tx(full, 2 * C::kStageBytes);
-                    tma_load_2d_pair(sa, amap, kin * kF8K, m0, full_leader);                                              // box {128 k, 128 rows}
-                    if (!P.adjoint) tma_load_2d_pair(sa + C::kABytes, wmap, kin * kF8K, nb0, full_leader);                // box {128 k, TN / 2 rows}
-                    else tma_load_2d_pair(sa + C::kABytes, wmap, nb0, kin * kF8K, full_leader);                           // box {TN / 2 columns, 128 k}
-                    if (++kin == P.kpw) {
-                        kin = 0;
-                        ++amap;
-                        wmap += wstep;
-                    }
-                    sa += C::kStageBytes;
-                    if (++s == C::kStages) {
-                        s = 0;
-                        sa = base;
-                        phase ^= 1;
+                uint32_t s = 0, phase = 0;
+                bool ok = true;
+                for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step) {
+                    const F8Tile t = F8Tile::of<TN>(P, tile);
+                    int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
+                    const int row = t.m0 + (int)prank * kF8Rows, column = t.n0 + (int)prank * (TN / 2);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        ok = f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag);
+                        if (!ok) break;
+                        const uint32_t full = bar_full + 8 * s, full_leader = map_to_cta(full, leader), sa = base + s * C::kStageBytes;
+                        const CUtensorMap *wmap = &P.w_map[P.adjoint ? r * P.pfi + t.oblk : t.oblk * P.pfi + r];
+                        if (prank == 0) mbar_expect_tx(full, 2 * C::kStageBytes);
+                        tma_load_2d_pair(sa, &P.a_map[r], kin * kF8K, row, full_leader);                                  // box {128 k, 128 rows}
+                        if (!P.adjoint) tma_load_2d_pair(sa + C::kABytes, wmap, kin * kF8K, column, full_leader);         // box {128 k, TN / 2 rows}
+                        else tma_load_2d_pair(sa + C::kABytes, wmap, column, kin * kF8K, full_leader);                    // box {TN / 2 columns, 128 k}
+                        if (++kin == P.kpw) {
+                            kin = 0;
+                            ++r;
+                        }
+                        if (++s == C::kStages) {
+                            s = 0;
+                            phase ^= 1;
+                        }
                     }
                 }
                 if (*abort_flag) {
@@ -235,7 +261,6 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     while (global_timer() - t0 < 1000000ull) {}
                 }
             }
-            __syncwarp();
         } else if (warp == 1) {
             if (lane == 0 && prank == 0) {
                 const uint32_t idesc = f8_instr(2 * kF8Rows, TN, 0, P.adjoint);
@@ -247,114 +272,165 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                 if (TN == 128 && P.adjoint) b0 = (b0 & ~((uint64_t)7 << 61)) | (uint64_t)4 << 61;
                 const uint64_t bstep = P.adjoint ? 32 * row >> 4 : 32 >> 4;
                 const uint16_t mask = (uint16_t)(3u << leader);
-                uint32_t s = 0, phase = 0;
-                uint64_t off = 0;
+                uint32_t s = 0, phase = 0, it = 0;
+                bool ok = true;
+                for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step)
+                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                        const uint32_t buf = it & 1u;
+                        ok = f8_wait(bar_free + 8 * buf, ((it >> 1) & 1u) ^ 1u, abort_flag) && f8_wait(bar_full + 8 * s, phase, abort_flag);
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                        const uint64_t off = (uint64_t)(s * (C::kStageBytes >> 4)), a = a0 + off, b = b0 + off;
+                        const uint32_t d = tmem + buf * TN;
+                        umma_f8_pair(d, a, b, idesc, 0u);
+                        umma_f8_pair(d, a + 2, b + bstep, idesc, 1u);
+                        umma_f8_pair(d, a + 4, b + 2 * bstep, idesc, 1u);
+                        umma_f8_pair(d, a + 6, b + 3 * bstep, idesc, 1u);
+                        tcgen05_commit_mask(bar_empty + 8 * s, mask);       // first: nobody retires before the sums are done
+                        tcgen05_commit_mask(bar_done + 8 * buf, mask);
+                        if (++s == C::kStages) {
+                            s = 0;
+                            phase ^= 1;
+                        }
+                    }
+            }
+        } else if (warp == 2) {
+            // scales: four rows a lane, and a weight block's by each of the first lanes, up to eight k-blocks ahead of the sums
+            uint32_t s = 0, phase = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step) {
+                const F8Tile t = F8Tile::of<TN>(P, tile);
+                int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
+                const int row0 = t.m0 + (int)prank * kF8Rows + lane, col = t.n0 + lane * kScaleBlock;
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    const uint32_t it = (uint32_t)(kb - kb0), buf = it & 1u;
-                    if (!f8_wait(bar_free + 8 * buf, ((it >> 1) & 1u) ^ 1u, abort_flag)) break;
-                    if (!f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
-                    tcgen05_fence_after();
-                    const uint64_t a = a0 + off, b = b0 + off;
-                    const uint32_t d = tmem + buf * TN;
-                    umma_f8_pair(d, a, b, idesc, 0u);
-                    umma_f8_pair(d, a + 2, b + bstep, idesc, 1u);
-                    umma_f8_pair(d, a + 4, b + 2 * bstep, idesc, 1u);
-                    umma_f8_pair(d, a + 6, b + 3 * bstep, idesc, 1u);
-                    tcgen05_commit_mask(bar_empty + 8 * s, mask);
-                    tcgen05_commit_mask(bar_done + 8 * buf, mask);
-                    off += C::kStageBytes >> 4;
-                    if (++s == C::kStages) {
+                    ok = __all_sync(0xffffffffu, f8_wait(bar_scale_free + 8 * s, phase ^ 1, abort_flag));
+                    if (!ok) break;
+                    const uint32_t slot = smem_u32(scales) + s * (kF8ScaleSlot * 4);
+                    const float *a = P.as[r] + (int64_t)kin * P.nb;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = row0 + 32 * i;
+                        copy_float_async(slot + 4 * (lane + 32 * i), a + min(row, P.nb - 1), row < P.nb);
+                    }
+                    if (lane < TN / kScaleBlock) {
+                        const float *w = P.ws[P.adjoint ? r * P.pfi + t.oblk : t.oblk * P.pfi + r] + (int64_t)kin * P.ws_k;
+                        copy_float_async(slot + 4 * (kF8Rows + lane), w + (col < P.blk_out ? (int64_t)(col / kScaleBlock) * P.ws_n : 0), col < P.blk_out);
+                    }
+                    arrive_after_copies(bar_scale + 8 * s);
+                    if (++kin == P.kpw) {
+                        kin = 0;
+                        ++r;
+                    }
+                    if (++s == kF8ScaleSlots) {
                         s = 0;
-                        off = 0;
                         phase ^= 1;
                     }
                 }
             }
-            __syncwarp();
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
         __syncwarp();
         tcgen05_fence_before();
         cluster_sync_all();
-        if (splits > 1) cluster_sync_all();
+        if (SPLIT) cluster_sync_all();
         if (warp == 1) {
             tcgen05_fence_after();
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * TN)) : "memory");
         }
     } else {
-        if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int quarter = warp & 3, half = (warp - 4) >> 2;               // tensor-memory lanes [32 q, 32 q + 32), columns [TN / 2 * half, ..)
-        const int row = m0 + quarter * 32 + lane, col = half * (TN / 2);
-        ScaleWalk walk(P, kb0, oblk, row, n0 + col);
-        uint64_t acc[TN / 4];
-#pragma unroll
-        for (int i = 0; i < TN / 4; ++i) acc[i] = 0ull;
-        constexpr int kAhead = 4;                                           // scales in flight
-        float next[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) next[i] = walk.next();
+        if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        const int quarter = warp & 3, col = ((warp - 4) >> 2) * 64;         // tensor-memory lanes [32 q, 32 q + 32), columns [col, col + 64)
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col;
         const uint32_t free_leader = map_to_cta(bar_free, leader);
+        const float *my_scale = scales + quarter * 32 + lane, *w_scale = scales + kF8Rows + col / kScaleBlock;
+        uint32_t slot = 0, sphase = 0, it = 0;
         bool ok = true;
-        for (int kb = kb0; ok && kb < kb1; kb += kAhead) {
+        for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step) {
+            float2 acc[32];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (kb + u >= kb1) break;
-                const uint32_t it = (uint32_t)(kb + u - kb0), buf = it & 1u;
+            for (int i = 0; i < 32; ++i) acc[i] = make_float2(0.f, 0.f);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t buf = it & 1u;
+                ok = __all_sync(0xffffffffu, f8_wait(bar_scale + 8 * slot, sphase, abort_flag));
+                if (!ok) break;
+                const float scale = my_scale[slot * kF8ScaleSlot] * w_scale[slot * kF8ScaleSlot];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_scale_free + 8 * slot);
+                if (++slot == kF8ScaleSlots) {
+                    slot = 0;
+                    sphase ^= 1;
+                }
                 ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, (it >> 1) & 1u, abort_flag));
                 if (!ok) break;
                 tcgen05_fence_after();
-                const uint64_t s = pair_of(next[u], next[u]);
-                next[u] = walk.next();
+                // two sums at an instruction
+                uint32_t v[32];
 #pragma unroll
-                for (int c = 0; c < TN / 2; c += 32) {
-                    uint64_t d[16];
-                    tmem_ld32_pairs(taddr + buf * TN + c, d);
-                    if (c + 32 == TN / 2) {                                 // this half of tensor memory may be written again
+                for (int c = 0; c < 2; ++c) {
+                    tmem_ld32(taddr + buf * TN + 32 * c, v);
+                    if (c == 1) {                                           // this half of tensor memory may be written again
                         tcgen05_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(free_leader + 8 * buf);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) fma_pair(acc[c / 2 + i], s, d[i]);
+                    for (int i = 0; i < 16; ++i)
+                        acc[16 * c + i] = __ffma2_rn(make_float2(scale, scale), make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), acc[16 * c + i]);
                 }
             }
-        }
-        // every product has been taken, so the ring is free: the sums as [row][column]
-        if (ok) {
-            float *o = reinterpret_cast<float *>(aligned) + (quarter * 32 + lane) * C::kPitch + col;
+            if (!ok) break;
+            const F8Tile t = F8Tile::of<TN>(P, tile);
+            const int m0 = t.m0 + (int)prank * kF8Rows;
+            const float *bias = P.bias[t.oblk];
+            if constexpr (!SPLIT) {
+                const int row = m0 + quarter * 32 + lane;
 #pragma unroll
-            for (int i = 0; i < TN / 4; i += 2) {
-                const float2 lo = floats_of(acc[i]), hi = floats_of(acc[i + 1]);
-                *reinterpret_cast<float4 *>(o + 2 * i) = make_float4(lo.x, lo.y, hi.x, hi.y);
-            }
-        }
-        tcgen05_fence_before();
-        cluster_sync_all();                                                 // every block's sums are in place
-        if (!*abort_flag) {
-            const int r0 = kF8Rows * split / splits, r1 = kF8Rows * (split + 1) / splits;
-            const float *bias = P.bias[oblk];
+                for (int c = 0; c < 64; c += 16) {
+                    const int column = t.n0 + col + c;
+                    if (column >= P.blk_out) continue;                      // whole groups of 16: blocks are multiples of that
+                    float o[16];
 #pragma unroll
-            for (int u = 0; u < TN / 128; ++u) {
-                const int c = 128 * u + 4 * lane, col = n0 + c;
-                if (col >= P.blk_out) continue;                                 // whole groups of four: blocks are multiples of 16
-                const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + col)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                for (int rl = r0 + warp - 4; rl < r1; rl += 8) {
-                    if (m0 + rl >= P.nb) break;
-                    const uint32_t addr = base + (uint32_t)((rl * C::kPitch + c) * 4);
-                    float4 v = ld_cluster_f4(map_to_cta(addr, prank));
-                    for (int q = 1; q < splits; ++q) {
-                        const float4 w = ld_cluster_f4(map_to_cta(addr, (uint32_t)(2 * q) + prank));
-                        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        const float2 lo = acc[(c + i) / 2], hi = acc[(c + i) / 2 + 1];
+                        o[i] = lo.x + b.x, o[i + 1] = lo.y + b.y, o[i + 2] = hi.x + b.z, o[i + 3] = hi.y + b.w;
                     }
-                    v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
-                    const int64_t at = (int64_t)(m0 + rl) * P.blk_out + col;
-                    if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[oblk]) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-                    else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[oblk]) + at) = v;
+                    if (row < P.nb) f8_store(P, t.oblk, (int64_t)row * P.blk_out + column, o);
+                }
+            } else {
+                // every product has been taken, so the ring is free: the sums as [row][column]
+                float *o = reinterpret_cast<float *>(aligned) + (quarter * 32 + lane) * C::kPitch + col;
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) *reinterpret_cast<float4 *>(o + 2 * i) = make_float4(acc[i].x, acc[i].y, acc[i + 1].x, acc[i + 1].y);
+                tcgen05_fence_before();
+                cluster_sync_all();                                         // every block's sums are in place
+                const int r0 = kF8Rows * split / splits, r1 = kF8Rows * (split + 1) / splits;
+#pragma unroll
+                for (int u = 0; u < TN / 128; ++u) {
+                    const int c = 128 * u + 4 * lane, column = t.n0 + c;
+                    if (column >= P.blk_out || *abort_flag) continue;
+                    const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                    for (int rl = r0 + warp - 4; rl < r1; rl += C::kSumWarps) {
+                        if (m0 + rl >= P.nb) break;
+                        const uint32_t addr = base + (uint32_t)((rl * C::kPitch + c) * 4);
+                        float4 v = ld_cluster_f4(map_to_cta(addr, prank));
+                        for (int q = 1; q < splits; ++q) {
+                            const float4 w = ld_cluster_f4(map_to_cta(addr, (uint32_t)(2 * q) + prank));
+                            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+                        }
+                        v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
+                        const int64_t at = (int64_t)(m0 + rl) * P.blk_out + column;
+                        if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[t.oblk]) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                        else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[t.oblk]) + at) = v;
+                    }
                 }
             }
         }
-        if (splits > 1) cluster_sync_all();                                 // nobody retires while a peer reads its shared memory
+        // A cluster whose waits ran out still meets at its barriers: once more here, and before the sums are read (SPLIT, above).
+        if (SPLIT && !ok) cluster_sync_all();
+        tcgen05_fence_before();
+        cluster_sync_all();                                                 // nobody retires while a peer uses its memory or its barriers
     }
 }
 
@@ -502,23 +578,24 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
         constexpr int kPer = (N + 31) / 32, kAhead = N >= 128 ? 2 : 4;
         float *mine = scales + quarter * 2 * N;
         int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
-        const auto fetch = [&](float *s) {                                  // the next k-block's scales, those of `lane`, `lane` + 32, ...
+        // the next k-block's scales, those of `lane`, `lane` + 32, ..., and the weights' one: multiplied when they are used, not waited for here
+        const auto fetch = [&](float *s, float &w) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) s[i] = 0.f;
             if (r >= P.nred) return;
-            const float w = __ldg(P.ws[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r] + (int64_t)kin * P.ws_k + (int64_t)(n0 / kScaleBlock) * P.ws_n);
+            w = __ldg(P.ws[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r] + (int64_t)kin * P.ws_k + (int64_t)(n0 / kScaleBlock) * P.ws_n);
             const float *a = P.as[r] + (int64_t)kin * P.nb;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (lane + 32 * i < P.nb) s[i] = __ldg(a + lane + 32 * i) * w;
+                if (lane + 32 * i < P.nb) s[i] = __ldg(a + lane + 32 * i);
             if (++kin == P.kpw) {
                 kin = 0;
                 ++r;
             }
         };
-        float next[kAhead][kPer];
+        float next[kAhead][kPer], wnext[kAhead] = {};
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) fetch(next[i]);
+        for (int i = 0; i < kAhead; ++i) fetch(next[i], wnext[i]);
         uint64_t acc[N / 2];
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) acc[i] = 0ull;
@@ -532,8 +609,8 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
                 float *set = mine + (u & 1) * N;
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
-                    if (N % 32 == 0 || lane + 32 * i < N) set[lane + 32 * i] = next[u][i];
-                fetch(next[u]);
+                    if (N % 32 == 0 || lane + 32 * i < N) set[lane + 32 * i] = next[u][i] * wnext[u];
+                fetch(next[u], wnext[u]);
                 __syncwarp();
                 ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, bphase, abort_flag));
                 if (!ok) break;
@@ -667,10 +744,13 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
     P.ws_n = adjoint ? 1 : scale_cols;
     P.adjoint = adjoint ? 1 : 0;
     P.out_bf16 = t == DISTDL_BF16;
+    P.nout = nout;
+    P.out_wide = 1;
     for (int i = 0; i < nact; ++i) P.as[i] = (const float *)act_scales[i];
     for (int i = 0; i < grid; ++i) P.ws[i] = (const float *)ws[i];
     for (int i = 0; i < nout; ++i) {
         P.out[i] = out[i];
+        if (reinterpret_cast<uintptr_t>(out[i]) & 31u) P.out_wide = 0;
         P.bias[i] = bias ? (const float *)bias[i] : nullptr;
     }
 
@@ -678,8 +758,10 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
     {
         std::lock_guard<std::mutex> setup_lock(setup_mutex());
         if (!configured_on[device]) {
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
             DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
             DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
             DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
@@ -724,10 +806,16 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
         else if (n == 64) launch_few<64>(P, tiles, sms, in);
         else launch_few<128>(P, tiles, sms, in);
     } else {
-        const int64_t blocks = row_tiles * nout * ((P.blk_out + tn - 1) / tn) * 2 * splits;
-        if (blocks > INT32_MAX) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
-        if (tn == 256) launch_clusters_in_stream(affine_fp8_pair_kernel<256>, 2u * splits, dim3((unsigned)blocks), dim3(kF8Threads), F8Cfg<256>::kSmemBytes, in, P);
-        else launch_clusters_in_stream(affine_fp8_pair_kernel<128>, 2u * splits, dim3((unsigned)blocks), dim3(kF8Threads), F8Cfg<128>::kSmemBytes, in, P);
+        const int64_t tiles = row_tiles * nout * ((P.blk_out + tn - 1) / tn);
+        if (tiles * 2 * splits > INT32_MAX / 2) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
+        P.tiles = (int32_t)tiles;
+        P.splits = splits;
+        const unsigned blocks = (unsigned)(splits > 1 ? tiles * 2 * splits : 2 * std::min<int64_t>(tiles, std::max(1, sms / 2)));
+        const auto launch = [&](auto kernel, unsigned threads, int smem) {
+            launch_clusters_in_stream(kernel, 2u * splits, dim3(blocks), dim3(threads), (size_t)smem, in, P);
+        };
+        if (tn == 256) launch(splits > 1 ? affine_fp8_pair_kernel<256, true> : affine_fp8_pair_kernel<256, false>, F8Cfg<256>::kThreads, F8Cfg<256>::kSmemBytes);
+        else launch(splits > 1 ? affine_fp8_pair_kernel<128, true> : affine_fp8_pair_kernel<128, false>, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes);
     }
     DISTDL_CUDA_CHECK(cudaGetLastError());
     return DISTDL_OK;
