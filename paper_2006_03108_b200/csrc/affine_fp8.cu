@@ -93,6 +93,14 @@ __device__ __forceinline__ float2 floats_of(uint64_t v) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
     return f;
 }
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+        : "r"(taddr) : "memory");
+}
 // 4 bytes, or four zeros, to shared memory, and an arrival at a barrier once this thread's copies so far are there.
 __device__ __forceinline__ void copy_float_async(uint32_t dst, const float *src, bool there) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4u : 0u) : "memory");
@@ -110,8 +118,10 @@ constexpr int kF8ScaleSlots = 8;                            // k-blocks whose sc
 constexpr int kF8ScaleSlot = kF8Rows + 8;                   // floats: the rows' scales, the two column halves' weight scales
 template <int TN>
 struct F8Cfg {
-    static constexpr int kSumWarps = TN / 64 * 4;           // 64 columns of 32 rows each
-    static constexpr int kThreads = 128 + 32 * kSumWarps;   // warp 0: TMA, warp 1: MMA and tensor memory, warp 2: scales, warps 4..: sums
+    static constexpr int kSumWarps = 8;                     // 32 rows and half of the columns each
+    static constexpr int kCols = TN / 2;
+    static constexpr int kBuffers = 512 / TN;               // products in tensor memory
+    static constexpr int kThreads = 128 + 32 * kSumWarps;   // warp 0: TMA, 1: MMA and tensor memory, 2: scales, 3: MMA, 4..: sums
     static constexpr int kABytes = kF8Rows * kF8K;          // 16 KB
     static constexpr int kBBytes = TN / 2 * kF8K;
     static constexpr int kStageBytes = kABytes + kBBytes;
@@ -121,7 +131,7 @@ struct F8Cfg {
     static constexpr int kSmemBytes = kStages * kStageBytes + kScaleBytes + kF8Tail;
     static_assert(kF8Rows * kPitch * 4 <= kStages * kStageBytes, "the sums take the ring's place");
     static_assert(TN % kScaleBlock == 0, "");
-    static constexpr int kBars = 2 * kStages + 4 + 2 * kF8ScaleSlots;
+    static constexpr int kBars = 2 * kStages + kBuffers + 2 * kF8ScaleSlots;
     static_assert(kBars * 8 + 8 <= 512, "barriers");
 };
 
@@ -184,10 +194,9 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     const float *scales = reinterpret_cast<const float *>(aligned + C::kStages * C::kStageBytes);
     uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + C::kStages * C::kStageBytes + C::kScaleBytes);
     const uint32_t bar_full = smem_u32(bars);
-    const uint32_t bar_empty = bar_full + 8 * C::kStages;
-    const uint32_t bar_done = bar_empty + 8 * C::kStages;   // two: a product of 128 is in tensor memory
-    const uint32_t bar_free = bar_done + 16;                // two: it has been taken
-    const uint32_t bar_scale = bar_free + 16;               // a k-block's scales are in shared memory
+    const uint32_t bar_done = bar_full + 8 * C::kStages;    // a stage's product of 128 is in tensor memory, and the stage is empty
+    const uint32_t bar_free = bar_done + 8 * C::kStages;    // a part of tensor memory has been read
+    const uint32_t bar_scale = bar_free + 8 * C::kBuffers;               // a k-block's scales are in shared memory
     const uint32_t bar_scale_free = bar_scale + 8 * kF8ScaleSlots;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -202,12 +211,9 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(bar_full + 8 * s, 1);
-            mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_done + 8 * s, 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(bar_done + 8 * b, 1);
-            mbar_init(bar_free + 8 * b, 2 * C::kSumWarps);  // the summing warps of both blocks
-        }
+        for (int b = 0; b < C::kBuffers; ++b) mbar_init(bar_free + 8 * b, 2 * C::kSumWarps);     // the summing warps of both blocks
         for (int s = 0; s < kF8ScaleSlots; ++s) {
             mbar_init(bar_scale + 8 * s, 32);               // the lanes that copy
             mbar_init(bar_scale_free + 8 * s, C::kSumWarps); // the summing warps
@@ -216,7 +222,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
         fence_barrier_init();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)(2 * TN)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tcgen05_fence_before();
@@ -224,10 +230,10 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // 256 columns: the launch gives all of the 640 threads 96 registers; the first four warps hand 64 of theirs over to the sixteen that hold the sums
-    // (32 + 4 * 112 = 5 * 96).
+    // 256 columns: a summing thread holds 128 sums.  The launch gives all of the 384 threads 168 registers; the first four warps hand 128 of theirs over to
+    // the eight that sum (40 + 2 * 232 = 3 * 168).
     if (warp < 4) {
-        if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
             if (lane == 0) {
                 uint32_t s = 0, phase = 0;
@@ -237,7 +243,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
                     const int row = t.m0 + (int)prank * kF8Rows, column = t.n0 + (int)prank * (TN / 2);
                     for (int kb = kb0; kb < kb1; ++kb) {
-                        ok = f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag);
+                        ok = f8_wait(bar_done + 8 * s, phase ^ 1, abort_flag);
                         if (!ok) break;
                         const uint32_t full = bar_full + 8 * s, full_leader = map_to_cta(full, leader), sa = base + s * C::kStageBytes;
                         const CUtensorMap *wmap = &P.w_map[P.adjoint ? r * P.pfi + t.oblk : t.oblk * P.pfi + r];
@@ -261,7 +267,9 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     while (global_timer() - t0 < 1000000ull) {}
                 }
             }
-        } else if (warp == 1) {
+        } else if (warp & 1) {
+            // Two warps issue products, every other one each: they are independent of one another, and a thread alone takes 750 clocks for the two waits,
+            // the four instructions and the commit of one, where the tensor cores take 300 to 600.
             if (lane == 0 && prank == 0) {
                 const uint32_t idesc = f8_instr(2 * kF8Rows, TN, 0, P.adjoint);
                 // K-major: 8-row groups 1024 bytes apart, a K step of 32 values is 32 bytes.  MN-major: rows of TN / 2 columns (128-byte swizzle, or 64-byte
@@ -272,27 +280,28 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                 if (TN == 128 && P.adjoint) b0 = (b0 & ~((uint64_t)7 << 61)) | (uint64_t)4 << 61;
                 const uint64_t bstep = P.adjoint ? 32 * row >> 4 : 32 >> 4;
                 const uint16_t mask = (uint16_t)(3u << leader);
-                uint32_t s = 0, phase = 0, it = 0;
-                bool ok = true;
-                for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step)
-                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                        const uint32_t buf = it & 1u;
-                        ok = f8_wait(bar_free + 8 * buf, ((it >> 1) & 1u) ^ 1u, abort_flag) && f8_wait(bar_full + 8 * s, phase, abort_flag);
-                        if (!ok) break;
-                        tcgen05_fence_after();
-                        const uint64_t off = (uint64_t)(s * (C::kStageBytes >> 4)), a = a0 + off, b = b0 + off;
-                        const uint32_t d = tmem + buf * TN;
-                        umma_f8_pair(d, a, b, idesc, 0u);
-                        umma_f8_pair(d, a + 2, b + bstep, idesc, 1u);
-                        umma_f8_pair(d, a + 4, b + 2 * bstep, idesc, 1u);
-                        umma_f8_pair(d, a + 6, b + 3 * bstep, idesc, 1u);
-                        tcgen05_commit_mask(bar_empty + 8 * s, mask);       // first: nobody retires before the sums are done
-                        tcgen05_commit_mask(bar_done + 8 * buf, mask);
-                        if (++s == C::kStages) {
-                            s = 0;
-                            phase ^= 1;
-                        }
+                static_assert(C::kStages % 2 == 0 && C::kBuffers % 2 == 0, "each of the two warps has stages and buffers of its own");
+                const uint32_t total = first_tile < P.tiles ? (uint32_t)((P.tiles - first_tile + tile_step - 1) / tile_step * (kb1 - kb0)) : 0u;
+                uint32_t s = (uint32_t)warp >> 1, phase = 0, buf = s, bphase = 1;
+                for (uint32_t it = s; it < total; it += 2) {
+                    if (!f8_wait(bar_free + 8 * buf, bphase, abort_flag) || !f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
+                    tcgen05_fence_after();
+                    const uint64_t off = (uint64_t)(s * (C::kStageBytes >> 4)), a = a0 + off, b = b0 + off;
+                    const uint32_t d = tmem + buf * TN;
+                    umma_f8_pair(d, a, b, idesc, 0u);
+                    umma_f8_pair(d, a + 2, b + bstep, idesc, 1u);
+                    umma_f8_pair(d, a + 4, b + 2 * bstep, idesc, 1u);
+                    umma_f8_pair(d, a + 6, b + 3 * bstep, idesc, 1u);
+                    tcgen05_commit_mask(bar_done + 8 * s, mask);
+                    if ((s += 2) >= C::kStages) {
+                        s -= C::kStages;
+                        phase ^= 1;
                     }
+                    if ((buf += 2) >= C::kBuffers) {
+                        buf -= C::kBuffers;
+                        bphase ^= 1;
+                    }
+                }
             }
         } else if (warp == 2) {
             // scales: four rows a lane, and a weight block's by each of the first lanes, up to eight k-blocks ahead of the sums
@@ -335,47 +344,57 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
         if (SPLIT) cluster_sync_all();
         if (warp == 1) {
             tcgen05_fence_after();
-            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * TN)) : "memory");
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
         }
     } else {
-        if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-        const int quarter = warp & 3, col = ((warp - 4) >> 2) * 64;         // tensor-memory lanes [32 q, 32 q + 32), columns [col, col + 64)
+        if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int quarter = warp & 3, col = ((warp - 4) >> 2) * C::kCols;   // tensor-memory lanes [32 q, 32 q + 32), columns from col
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col;
         const uint32_t free_leader = map_to_cta(bar_free, leader);
         const float *my_scale = scales + quarter * 32 + lane, *w_scale = scales + kF8Rows + col / kScaleBlock;
-        uint32_t slot = 0, sphase = 0, it = 0;
+        uint32_t s = 0, phase = 0, it = 0, slot = 0, sphase = 0;
+        float scale = 0.f;
+        // the scale of the next k-block
+        const auto next_scale = [&]() {
+            if (!__all_sync(0xffffffffu, f8_wait(bar_scale + 8 * slot, sphase, abort_flag))) return false;
+            scale = my_scale[slot * kF8ScaleSlot] * w_scale[slot * kF8ScaleSlot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_scale_free + 8 * slot);
+            if (++slot == kF8ScaleSlots) {
+                slot = 0;
+                sphase ^= 1;
+            }
+            return true;
+        };
         bool ok = true;
         for (int tile = first_tile; ok && tile < P.tiles; tile += tile_step) {
-            float2 acc[32];
+            float2 acc[C::kCols / 2];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] = make_float2(0.f, 0.f);
+            for (int i = 0; i < C::kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t buf = it & 1u;
-                ok = __all_sync(0xffffffffu, f8_wait(bar_scale + 8 * slot, sphase, abort_flag));
-                if (!ok) break;
-                const float scale = my_scale[slot * kF8ScaleSlot] * w_scale[slot * kF8ScaleSlot];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_scale_free + 8 * slot);
-                if (++slot == kF8ScaleSlots) {
-                    slot = 0;
-                    sphase ^= 1;
-                }
-                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, (it >> 1) & 1u, abort_flag));
+                const uint32_t buf = it % C::kBuffers;
+                if (!(ok = next_scale())) break;
+                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * s, phase, abort_flag));
                 if (!ok) break;
                 tcgen05_fence_after();
-                // two sums at an instruction
-                uint32_t v[32];
+                const float now = scale;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    tmem_ld32(taddr + buf * TN + 32 * c, v);
-                    if (c == 1) {                                           // this half of tensor memory may be written again
+                for (int c = 0; c < C::kCols; c += 64) {
+                    uint32_t v[64];
+                    tmem_ld64(taddr + buf * TN + c, v);
+                    if (c + 64 == C::kCols) {                               // this part of tensor memory may be written again
                         tcgen05_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(free_leader + 8 * buf);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[16 * c + i] = __ffma2_rn(make_float2(scale, scale), make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), acc[16 * c + i]);
+                    for (int i = 0; i < 32; ++i)                            // two sums at an instruction
+                        acc[c / 2 + i] = __ffma2_rn(make_float2(now, now), make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), acc[c / 2 + i]);
+                }
+                if (!ok) break;
+                if (++s == C::kStages) {
+                    s = 0;
+                    phase ^= 1;
                 }
             }
             if (!ok) break;
@@ -385,7 +404,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
             if constexpr (!SPLIT) {
                 const int row = m0 + quarter * 32 + lane;
 #pragma unroll
-                for (int c = 0; c < 64; c += 16) {
+                for (int c = 0; c < C::kCols; c += 16) {
                     const int column = t.n0 + col + c;
                     if (column >= P.blk_out) continue;                      // whole groups of 16: blocks are multiples of that
                     float o[16];
@@ -401,7 +420,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                 // every product has been taken, so the ring is free: the sums as [row][column]
                 float *o = reinterpret_cast<float *>(aligned) + (quarter * 32 + lane) * C::kPitch + col;
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) *reinterpret_cast<float4 *>(o + 2 * i) = make_float4(acc[i].x, acc[i].y, acc[i + 1].x, acc[i + 1].y);
+                for (int i = 0; i < C::kCols / 2; i += 2) *reinterpret_cast<float4 *>(o + 2 * i) = make_float4(acc[i].x, acc[i].y, acc[i + 1].x, acc[i + 1].y);
                 tcgen05_fence_before();
                 cluster_sync_all();                                         // every block's sums are in place
                 const int r0 = kF8Rows * split / splits, r1 = kF8Rows * (split + 1) / splits;
@@ -410,19 +429,26 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     const int c = 128 * u + 4 * lane, column = t.n0 + c;
                     if (column >= P.blk_out || *abort_flag) continue;
                     const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                    for (int rl = r0 + warp - 4; rl < r1; rl += C::kSumWarps) {
-                        if (m0 + rl >= P.nb) break;
-                        const uint32_t addr = base + (uint32_t)((rl * C::kPitch + c) * 4);
-                        float4 v = ld_cluster_f4(map_to_cta(addr, prank));
+                    for (int rl = r0 + warp - 4; rl < r1; rl += 4 * C::kSumWarps) {
+                        float4 v[4];                                        // four rows in flight; S divides 32, so they are there
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = ld_cluster_f4(map_to_cta(base + (uint32_t)(((rl + i * C::kSumWarps) * C::kPitch + c) * 4), prank));
                         for (int q = 1; q < splits; ++q) {
-                            const float4 w = ld_cluster_f4(map_to_cta(addr, (uint32_t)(2 * q) + prank));
-                            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+                            float4 w[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) w[i] = ld_cluster_f4(map_to_cta(base + (uint32_t)(((rl + i * C::kSumWarps) * C::kPitch + c) * 4), (uint32_t)(2 * q) + prank));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i].x += w[i].x, v[i].y += w[i].y, v[i].z += w[i].z, v[i].w += w[i].w;
                         }
-                        v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
-                        const int64_t at = (int64_t)(m0 + rl) * P.blk_out + column;
-                        if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[t.oblk]) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-                        else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[t.oblk]) + at) = v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int row = m0 + rl + i * C::kSumWarps;
+                            if (row >= P.nb) continue;
+                            v[i].x += b.x, v[i].y += b.y, v[i].z += b.z, v[i].w += b.w;
+                            const int64_t at = (int64_t)row * P.blk_out + column;
+                            if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[t.oblk]) + at) = make_uint2(pack_bf16(v[i].x, v[i].y), pack_bf16(v[i].z, v[i].w));
+                            else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[t.oblk]) + at) = v[i];
+                        }
                     }
                 }
             }
