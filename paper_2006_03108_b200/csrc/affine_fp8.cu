@@ -79,20 +79,7 @@ __host__ __device__ constexpr uint32_t f8_instr(int m, int n, int a_mn, int b_mn
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
-// acc += s * d for pairs of floats
-__device__ __forceinline__ void fma_pair(uint64_t &acc, uint64_t s, uint64_t d) {
-    asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(s), "l"(d));
-}
-__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 floats_of(uint64_t v) {
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-    return f;
-}
+// 64 columns of tensor memory, and the wait for them.
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *v) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
@@ -133,6 +120,8 @@ struct F8Cfg {
     static_assert(TN % kScaleBlock == 0, "");
     static constexpr int kBars = 2 * kStages + kBuffers + 2 * kF8ScaleSlots;
     static_assert(kBars * 8 + 8 <= 512, "barriers");
+    // a stage's next product waits for the sums to have taken its last one: its barrier is never two turns ahead of them
+    static_assert(kStages >= kBuffers, "as many stages as products");
 };
 
 // Tiles in groups of eight rows of tiles, column by column inside a group, so that what runs at a time shares its rows and columns in L2.
@@ -462,10 +451,9 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
 
 // ------------------------------------------------------------------------------------------
 // Few samples (a batch of at most 128): the weights are the M operand, 128 output features a block, the batch takes N = 16, 32, 64 or 128 columns.  A
-// cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds it is the stream of
-// the weights; two blocks an SM keep it going.
+// cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds
+// it is the stream of the weights: two blocks an SM (one for N = 128) keep it going, and its first copies leave before anything else is set up.
 // ------------------------------------------------------------------------------------------
-constexpr int kF8FewThreads = 192;                          // warp 0: TMA, warp 1: MMA and tensor memory, warps 2..5: sums
 constexpr int kF8WBytes = 128 * kF8K;
 constexpr int kF8FewMaxStages = 12;
 constexpr int kF8FewMaxSmem = 220 * 1024;                   // one block an SM; half of it: two
@@ -476,17 +464,31 @@ struct AffineF8FewParams {
 };
 template <int N>
 struct F8FewCfg {
+    static constexpr int kParts = N >= 128 ? 2 : 1;         // summing warps: four for each part of the columns
+    static constexpr int kCols = N / kParts;
+    static constexpr int kThreads = 128 + 128 * kParts;     // warp 0: TMA, 1: MMA and tensor memory, 3: MMA, 4..: sums
+    static constexpr int kBlocksPerSm = N >= 128 ? 1 : 2;
+    static constexpr int kLoad = N == 32 ? 32 : N >= 128 ? 64 : 16;         // columns that a tensor-memory load takes: what registers allow
     static constexpr int kStageBytes = kF8WBytes + N * kF8K;
-    static constexpr int kBuffers = N >= 128 ? 2 : N >= 64 ? 4 : 8;         // products in tensor memory
+    static constexpr int kBuffers = N >= 128 ? 2 : 4;       // products in tensor memory
     static constexpr int kTmemCols = kBuffers * N;
-    static constexpr int kMinStages = N >= 64 ? 3 : 2;                      // room for the sums: 512 N bytes
-    static constexpr int kScaleBytes = 4 * 2 * N * 4;                       // two sets of a k-block's scales for each of four warps
+    static constexpr int kScaleBytes = 4 * kParts * 2 * kCols * 4;          // two sets of a k-block's scales for each summing warp
     static constexpr int kTail = kF8Tail + kScaleBytes;
-    static_assert(kMinStages * kStageBytes >= 512 * N, "the sums take the ring's place");
+    static constexpr int kMinStages = (512 * N + kStageBytes - 1) / kStageBytes;      // the sums take the ring's place
+    static_assert((2 * kF8FewMaxStages + kBuffers) * 8 + 8 <= 512, "barriers");
+    static_assert((kF8FewMaxSmem / kBlocksPerSm - kTail) / kStageBytes >= kMinStages, "room for the sums");
+    // a stage's next product waits for the sums to have taken its last one: its barrier is never two turns ahead of them
+    static_assert((kF8FewMaxSmem / kBlocksPerSm - kTail) / kStageBytes >= kBuffers, "as many stages as products");
 };
+template <int C>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t *v) {
+    if constexpr (C == 16) tmem_ld16(taddr, v);
+    else if constexpr (C == 32) tmem_ld32(taddr, v);
+    else tmem_ld64(taddr, v);
+}
 
 template <int N>
-__global__ void __launch_bounds__(kF8FewThreads, 2)
+__global__ void __launch_bounds__(F8FewCfg<N>::kThreads, F8FewCfg<N>::kBlocksPerSm)
 affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
     stream_enter();
     using C = F8FewCfg<N>;
@@ -498,10 +500,9 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
     float *scales = reinterpret_cast<float *>(aligned + Q.stages * C::kStageBytes);
     uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + Q.stages * C::kStageBytes + C::kScaleBytes);
     const uint32_t bar_full = smem_u32(bars);
-    const uint32_t bar_empty = bar_full + 8 * kF8FewMaxStages;
-    __shared__ __align__(8) uint64_t turn[2 * C::kBuffers];
-    const uint32_t bar_done = smem_u32(turn), bar_free = bar_done + 8 * C::kBuffers;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * kF8FewMaxStages);
+    const uint32_t bar_done = bar_full + 8 * kF8FewMaxStages;       // a stage's product is in tensor memory, and the stage is empty
+    const uint32_t bar_free = bar_done + 8 * kF8FewMaxStages;       // a part of tensor memory has been read
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * kF8FewMaxStages + C::kBuffers);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -512,18 +513,27 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
     const int n0 = (tile - oblk * tiles_per_block) * 128;   // first output feature inside the block
     const int all = P.nred * P.kpw;
     const int kb0 = (int)((int64_t)all * rank / Q.split), kb1 = (int)((int64_t)all * (rank + 1) / Q.split);
+    const int stages = Q.stages;
 
+    // one k-block's copies
+    const auto copy = [&](int kb, uint32_t s) {
+        const int r = kb / P.kpw, k = (kb - r * P.kpw) * kF8K;
+        const uint32_t full = bar_full + 8 * s, sa = base + s * C::kStageBytes;
+        const CUtensorMap *wmap = &P.w_map[P.adjoint ? r * P.pfi + oblk : oblk * P.pfi + r];
+        mbar_expect_tx(full, C::kStageBytes);
+        if (!P.adjoint) tma_load_2d(sa, wmap, k, n0, full);                                // K-major: box {128 k, 128 features}
+        else tma_load_2d(sa, wmap, n0, k, full);                                           // MN-major: box {128 features, 128 k}
+        tma_load_2d(sa + kF8WBytes, &P.a_map[r], k, 0, full);                              // box {128 k, N rows}
+    };
     if (threadIdx.x == 0) {
-        for (int s = 0; s < Q.stages; ++s) {
+        for (int s = 0; s < stages; ++s) {
             mbar_init(bar_full + 8 * s, 1);
-            mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_done + 8 * s, 1);
         }
-        for (int b = 0; b < C::kBuffers; ++b) {
-            mbar_init(bar_done + 8 * b, 1);
-            mbar_init(bar_free + 8 * b, 4);
-        }
+        for (int b = 0; b < C::kBuffers; ++b) mbar_init(bar_free + 8 * b, 4 * C::kParts);
         *abort_flag = 0;
         fence_barrier_init();
+        for (int kb = kb0; kb < min(kb1, kb0 + stages); ++kb) copy(kb, (uint32_t)(kb - kb0));
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)C::kTmemCols) : "memory");
@@ -536,26 +546,12 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
 
     if (warp == 0) {
         if (lane == 0) {
-            int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
-            const int wstep = P.adjoint ? P.pfi : 1;
-            const CUtensorMap *wmap = (P.adjoint ? &P.w_map[oblk] : &P.w_map[oblk * P.pfi]) + r * wstep;
-            uint32_t s = 0, phase = 0, sa = base;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!f8_wait(bar_empty + 8 * s, phase ^ 1, abort_flag)) break;
-                const uint32_t full = bar_full + 8 * s;
-                mbar_expect_tx(full, C::kStageBytes);
-                if (!P.adjoint) tma_load_2d(sa, wmap, kin * kF8K, n0, full);               // K-major: box {128 k, 128 features}
-                else tma_load_2d(sa, wmap, n0, kin * kF8K, full);                          // MN-major: box {128 features, 128 k}
-                tma_load_2d(sa + kF8WBytes, &P.a_map[r], kin * kF8K, 0, full);             // box {128 k, N rows}
-                if (++kin == P.kpw) {
-                    kin = 0;
-                    ++r;
-                    wmap += wstep;
-                }
-                sa += C::kStageBytes;
-                if (++s == (uint32_t)Q.stages) {
+            uint32_t s = 0, phase = 0;
+            for (int kb = kb0 + stages; kb < kb1; ++kb) {
+                if (!f8_wait(bar_done + 8 * s, phase, abort_flag)) break;
+                copy(kb, s);
+                if (++s == (uint32_t)stages) {
                     s = 0;
-                    sa = base;
                     phase ^= 1;
                 }
             }
@@ -565,46 +561,41 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
             }
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp < 4 && (warp & 1)) {
+        // two warps issue products, every other one each (see the pair kernel)
         if (lane == 0) {
             const uint32_t idesc = f8_instr(128, N, P.adjoint, 0);
             const uint64_t a0 = smem_desc(base, P.adjoint ? kF8WBytes : 16, 1024);
             const uint64_t astep = P.adjoint ? 32 * 128 >> 4 : 32 >> 4;
             const uint64_t b0 = smem_desc(base + kF8WBytes, 16, 1024);
-            uint32_t s = 0, phase = 0, buf = 0, bphase = 0;
-            uint64_t off = 0;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!f8_wait(bar_free + 8 * buf, bphase ^ 1, abort_flag)) break;
-                if (!f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
+            uint32_t s = (uint32_t)warp >> 1, phase = 0, buf = s, bphase = 1;
+            if (s >= (uint32_t)stages) s -= stages, phase ^= 1;
+            for (int kb = kb0 + (warp >> 1); kb < kb1; kb += 2) {
+                if (!f8_wait(bar_free + 8 * buf, bphase, abort_flag) || !f8_wait(bar_full + 8 * s, phase, abort_flag)) break;
                 tcgen05_fence_after();
-                const uint64_t a = a0 + off, b = b0 + off;
+                const uint64_t off = (uint64_t)(s * (C::kStageBytes >> 4)), a = a0 + off, b = b0 + off;
                 const uint32_t d = tmem + buf * N;
                 umma_f8(d, a, b, idesc, 0u);
                 umma_f8(d, a + astep, b + 2, idesc, 1u);
                 umma_f8(d, a + 2 * astep, b + 4, idesc, 1u);
                 umma_f8(d, a + 3 * astep, b + 6, idesc, 1u);
-                tcgen05_commit(bar_empty + 8 * s);
-                tcgen05_commit(bar_done + 8 * buf);
-                off += C::kStageBytes >> 4;
-                if (++s == (uint32_t)Q.stages) {
-                    s = 0;
-                    off = 0;
-                    phase ^= 1;
-                }
-                if (++buf == C::kBuffers) {
-                    buf = 0;
+                tcgen05_commit(bar_done + 8 * s);
+                s += 2;
+                while (s >= (uint32_t)stages) s -= stages, phase ^= 1;
+                if ((buf += 2) >= C::kBuffers) {
+                    buf -= C::kBuffers;
                     bphase ^= 1;
                 }
             }
         }
         __syncwarp();
-    } else {
+    } else if (warp >= 4) {
         // A lane is a feature; the samples' scales, times the weights' one, go through shared memory of the warp's own, two sets in turn.
-        const int quarter = warp & 3;
-        constexpr int kPer = (N + 31) / 32, kAhead = N >= 128 ? 2 : 4;
-        float *mine = scales + quarter * 2 * N;
+        const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * C::kCols;
+        constexpr int kPer = (C::kCols + 31) / 32, kAhead = 4;
+        float *mine = scales + (warp - 4) * 2 * C::kCols;
         int r = kb0 / P.kpw, kin = kb0 - r * P.kpw;
-        // the next k-block's scales, those of `lane`, `lane` + 32, ..., and the weights' one: multiplied when they are used, not waited for here
+        // the next k-block's scales, those of columns `lane`, `lane` + 32, ..., and the weights' one: multiplied when they are used, not waited for here
         const auto fetch = [&](float *s, float &w) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) s[i] = 0.f;
@@ -613,7 +604,7 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
             const float *a = P.as[r] + (int64_t)kin * P.nb;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (lane + 32 * i < P.nb) s[i] = __ldg(a + lane + 32 * i);
+                if (col0 + lane + 32 * i < P.nb) s[i] = __ldg(a + col0 + lane + 32 * i);
             if (++kin == P.kpw) {
                 kin = 0;
                 ++r;
@@ -622,55 +613,56 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
         float next[kAhead][kPer], wnext[kAhead] = {};
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(next[i], wnext[i]);
-        uint64_t acc[N / 2];
+        float2 acc[C::kCols / 2];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) acc[i] = 0ull;
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
-        uint32_t buf = 0, bphase = 0;
+        for (int i = 0; i < C::kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
+        uint32_t s = 0, phase = 0, buf = 0;
         bool ok = true;
         for (int kb = kb0; ok && kb < kb1; kb += kAhead) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (kb + u >= kb1) break;
-                float *set = mine + (u & 1) * N;
+                float *set = mine + (u & 1) * C::kCols;
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
-                    if (N % 32 == 0 || lane + 32 * i < N) set[lane + 32 * i] = next[u][i] * wnext[u];
+                    if (C::kCols % 32 == 0 || lane + 32 * i < C::kCols) set[lane + 32 * i] = next[u][i] * wnext[u];
                 fetch(next[u], wnext[u]);
                 __syncwarp();
-                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * buf, bphase, abort_flag));
+                ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * s, phase, abort_flag));
                 if (!ok) break;
                 tcgen05_fence_after();
 #pragma unroll
-                for (int c = 0; c < N; c += 16) {
-                    uint32_t v[16];
-                    tmem_ld16(taddr + buf * N + c, v);
-                    if (c + 16 == N) {
+                for (int c = 0; c < C::kCols; c += C::kLoad) {
+                    uint32_t v[C::kLoad];
+                    tmem_ld<C::kLoad>(taddr + buf * N + c, v);
+                    if (c + C::kLoad == C::kCols) {
                         tcgen05_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar_free + 8 * buf);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const float4 s = *reinterpret_cast<const float4 *>(set + c + i);
-                        fma_pair(acc[(c + i) / 2], pair_of(s.x, s.y), (uint64_t)v[i] | (uint64_t)v[i + 1] << 32);
-                        fma_pair(acc[(c + i) / 2 + 1], pair_of(s.z, s.w), (uint64_t)v[i + 2] | (uint64_t)v[i + 3] << 32);
+                    for (int i = 0; i < C::kLoad; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(set + c + i);
+                        float2 &lo = acc[(c + i) / 2], &hi = acc[(c + i) / 2 + 1];
+                        lo = __ffma2_rn(make_float2(f.x, f.y), make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), lo);
+                        hi = __ffma2_rn(make_float2(f.z, f.w), make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), hi);
                     }
                 }
-                if (++buf == C::kBuffers) {
-                    buf = 0;
-                    bphase ^= 1;
+                if (++s == (uint32_t)stages) {
+                    s = 0;
+                    phase ^= 1;
                 }
+                if (++buf == C::kBuffers) buf = 0;
             }
         }
-        // the blocks' other warps have no use for the ring once every product has been taken: the sums as [sample][feature]
+        // every product has been taken, so the ring is free: the sums as [sample][feature]
         if (ok) {
-            float *part = reinterpret_cast<float *>(aligned) + quarter * 32 + lane;
+            float *part = reinterpret_cast<float *>(aligned) + col0 * 128 + quarter * 32 + lane;
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                const float2 f = floats_of(acc[i]);
-                part[(2 * i) * 128] = f.x;
-                part[(2 * i + 1) * 128] = f.y;
+            for (int i = 0; i < C::kCols / 2; ++i) {
+                part[(2 * i) * 128] = acc[i].x;
+                part[(2 * i + 1) * 128] = acc[i].y;
             }
         }
     }
@@ -681,7 +673,7 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
         const int f = 4 * lane;
         if (n0 + f < P.blk_out) {
             const float4 bias = P.bias[oblk] ? __ldg(reinterpret_cast<const float4 *>(P.bias[oblk] + n0 + f)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int row = row0 + warp; row < row1; row += kF8FewThreads / 32) {
+            for (int row = row0 + warp; row < row1; row += C::kThreads / 32) {
                 const uint32_t addr = base + (uint32_t)((row * 128 + f) * 4);
                 float4 o = ld_cluster_f4(map_to_cta(addr, 0));
                 for (int q = 1; q < Q.split; ++q) {
@@ -718,19 +710,38 @@ static bool make_map_u8(CUtensorMap *m, const void *ptr, int64_t rows, int64_t c
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of 256 or 128 columns, the contraction in one, two or four runs: the one with the least time by its clusters' turns.  Measured (B200, us): the
+// first tile without its k-blocks, each further one (a pair goes on while sums are written), a k-block.  The narrow tile reads a half more through L2 for the same
+// work, but fills SMs that wide ones leave idle; so do runs, which cost a meeting of their blocks (256 x 8192 x 8192: 256 columns in 1, 2, 4 runs 33.6, 24.9, 52.4;
+// 128 columns 25.4, 33.8, 63.3.  2048 x 8192 x 8192: 127, 180, 295; 151, 256, 425.  200 x 8192 x 1024: 31.4, 21.5, 16.4; 24.4, 16.0, 12.6).
+struct F8Shape {
+    void (*kernel)(AffineF8Params);
+    int tn, splits, threads, smem;
+    double first, next, kblock;
+};
+constexpr int kF8Shapes = 6;
+static const F8Shape kF8Shape[kF8Shapes] = {
+    {affine_fp8_pair_kernel<256, false>, 256, 1, F8Cfg<256>::kThreads, F8Cfg<256>::kSmemBytes, 6.2, 1.8, 0.44},
+    {affine_fp8_pair_kernel<256, true>, 256, 2, F8Cfg<256>::kThreads, F8Cfg<256>::kSmemBytes, 8.3, 0.0, 0.48},
+    {affine_fp8_pair_kernel<256, true>, 256, 4, F8Cfg<256>::kThreads, F8Cfg<256>::kSmemBytes, 10.1, 0.0, 0.48},
+    {affine_fp8_pair_kernel<128, false>, 128, 1, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes, 5.1, 1.2, 0.31},
+    {affine_fp8_pair_kernel<128, true>, 128, 2, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes, 6.5, 0.0, 0.32},
+    {affine_fp8_pair_kernel<128, true>, 128, 4, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes, 7.8, 0.0, 0.32},
+};
+
 template <int N>
-static distdl_status_t launch_few(const AffineF8Params &P, int64_t tiles, int sms, cudaStream_t stream) {
-    // blocks of a tile: doubled while twice as many blocks as SMs are not exceeded and every block keeps four k-blocks
+static void launch_few(const AffineF8Params &P, int64_t tiles, int sms, cudaStream_t stream) {
+    // blocks of a tile: doubled while the device holds them all at a time and every block keeps four k-blocks
+    using C = F8FewCfg<N>;
     AffineF8FewParams Q;
     Q.p = P;
     Q.split = 1;
     const int64_t all = (int64_t)P.nred * P.kpw;
-    while (Q.split < 8 && tiles * Q.split * 2 <= 2 * sms && all >= 4 * 2 * Q.split) Q.split *= 2;
-    const int budget = tiles * Q.split <= sms ? kF8FewMaxSmem : kF8FewMaxSmem / 2;
-    Q.stages = std::min(kF8FewMaxStages, (budget - F8FewCfg<N>::kTail) / F8FewCfg<N>::kStageBytes);
-    const int smem = Q.stages * F8FewCfg<N>::kStageBytes + F8FewCfg<N>::kTail;
-    launch_clusters_in_stream(affine_fp8_few_kernel<N>, (unsigned)Q.split, dim3((unsigned)(tiles * Q.split)), dim3(kF8FewThreads), (size_t)smem, stream, Q);
-    return DISTDL_OK;
+    while (Q.split < 8 && tiles * Q.split * 2 <= C::kBlocksPerSm * sms && all >= 4 * 2 * Q.split) Q.split *= 2;
+    const int budget = C::kBlocksPerSm == 1 || tiles * Q.split <= sms ? kF8FewMaxSmem : kF8FewMaxSmem / 2;
+    Q.stages = std::min(kF8FewMaxStages, (budget - C::kTail) / C::kStageBytes);
+    const int smem = Q.stages * C::kStageBytes + C::kTail;
+    launch_clusters_in_stream(affine_fp8_few_kernel<N>, (unsigned)Q.split, dim3((unsigned)(tiles * Q.split)), dim3(C::kThreads), (size_t)smem, stream, Q);
 }
 
 static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *act, const void *const *act_scales,
@@ -780,68 +791,75 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
         P.bias[i] = bias ? (const float *)bias[i] : nullptr;
     }
 
+    // one-time set-up per device: kernel attributes, and how many clusters of each kind run at a time
     static bool configured_on[kMaxDevicesPerProcess] = {false};
+    static int clusters_on[kMaxDevicesPerProcess][kF8Shapes];
     {
         std::lock_guard<std::mutex> setup_lock(setup_mutex());
         if (!configured_on[device]) {
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<256, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<256>::kSmemBytes));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_pair_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Cfg<128>::kSmemBytes));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
-            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(affine_fp8_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+            for (int i = 0; i < kF8Shapes; ++i) {
+                const F8Shape &s = kF8Shape[i];
+                DISTDL_CUDA_CHECK(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
+                cudaLaunchConfig_t cfg = {};
+                cfg.gridDim = dim3((unsigned)(2 * s.splits * sms));
+                cfg.blockDim = dim3((unsigned)s.threads);
+                cfg.dynamicSmemBytes = (size_t)s.smem;
+                cudaLaunchAttribute attr = {};
+                attr.id = cudaLaunchAttributeClusterDimension;
+                attr.val.clusterDim.x = 2u * s.splits;
+                attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+                cfg.attrs = &attr;
+                cfg.numAttrs = 1;
+                DISTDL_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&clusters_on[device][i], s.kernel, &cfg));
+            }
+            for (const auto kernel : {affine_fp8_few_kernel<16>, affine_fp8_few_kernel<32>, affine_fp8_few_kernel<64>, affine_fp8_few_kernel<128>})
+                DISTDL_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
             configured_on[device] = true;
         }
     }
     const bool few = nb <= kF8Rows;
     const int n = nb <= 16 ? 16 : nb <= 32 ? 32 : nb <= 64 ? 64 : 128;
-    // tile width and splits of the contraction: fewest clocks by a count of turns (see the measured clocks of a k-block below)
-    int tn = 256, splits = 1;
     const int64_t row_tiles = (nb + 2 * kF8Rows - 1) / (2 * kF8Rows), all = (int64_t)P.nred * P.kpw;
+    const F8Shape *shape = nullptr;
+    int64_t tiles = 0, at_once = 1;
     if (!few) {
         double best = 0;
-        for (int width : {256, 128})
-            for (int s : {1, 2, 4}) {
-                if (s > 1 && all < 8 * s) continue;
-                const int64_t tiles = row_tiles * nout * ((P.blk_out + width - 1) / width);
-                const int64_t at_once = std::max(1, sms / (2 * s)), turns = (tiles + at_once - 1) / at_once;
-                const double clocks = (double)turns * ((double)((all + s - 1) / s) * (width == 256 ? 600 : 400) + (width == 256 ? 5000 : 3500) + (s > 1 ? 1000 * s : 0));
-                if (best == 0 || clocks < best) {
-                    best = clocks;
-                    tn = width;
-                    splits = s;
-                }
+        for (int i = 0; i < kF8Shapes; ++i) {
+            const F8Shape &s = kF8Shape[i];
+            if ((s.splits > 1 && all < 4 * s.splits) || clusters_on[device][i] < 1) continue;
+            const int64_t n_tiles = row_tiles * nout * ((P.blk_out + s.tn - 1) / s.tn), turns = (n_tiles + clusters_on[device][i] - 1) / clusters_on[device][i];
+            const double us = s.first + (double)turns * (double)((all + s.splits - 1) / s.splits) * s.kblock + (double)(turns - 1) * (s.splits > 1 ? s.first : s.next);
+            if (!shape || us < best) {
+                best = us;
+                shape = &s;
+                tiles = n_tiles;
+                at_once = clusters_on[device][i];
             }
+        }
+        if (!shape) return fail(DISTDL_ERR_CUDA, "%s: no cluster of two blocks fits the device", what);
     }
     for (int i = 0; i < nact; ++i)
         if (!make_map_u8(&P.a_map[i], act[i], nb, P.blk_red, kF8K, few ? n : kF8Rows))
             return fail(DISTDL_ERR_CUDA, "%s: tensor map of activation block %d failed", what, i);
     for (int i = 0; i < grid; ++i) {
         // weights: the columns of a tile that a block stages, by 128 of the contraction
-        const int columns = few ? 128 : tn / 2;
+        const int columns = few ? 128 : shape->tn / 2;
         const bool ok = adjoint ? make_map_u8(&P.w_map[i], w[i], bfo, bfi, columns, kF8K) : make_map_u8(&P.w_map[i], w[i], bfo, bfi, kF8K, columns);
         if (!ok) return fail(DISTDL_ERR_CUDA, "%s: tensor map of weight block %d failed", what, i);
     }
     const cudaStream_t in = (cudaStream_t)stream;
     if (few) {
-        const int64_t tiles = nout * scale_blocks(P.blk_out);
+        tiles = nout * scale_blocks(P.blk_out);
         if (n == 16) launch_few<16>(P, tiles, sms, in);
         else if (n == 32) launch_few<32>(P, tiles, sms, in);
         else if (n == 64) launch_few<64>(P, tiles, sms, in);
         else launch_few<128>(P, tiles, sms, in);
     } else {
-        const int64_t tiles = row_tiles * nout * ((P.blk_out + tn - 1) / tn);
-        if (tiles * 2 * splits > INT32_MAX / 2) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
+        if (tiles * 2 * shape->splits > INT32_MAX / 2) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
         P.tiles = (int32_t)tiles;
-        P.splits = splits;
-        const unsigned blocks = (unsigned)(splits > 1 ? tiles * 2 * splits : 2 * std::min<int64_t>(tiles, std::max(1, sms / 2)));
-        const auto launch = [&](auto kernel, unsigned threads, int smem) {
-            launch_clusters_in_stream(kernel, 2u * splits, dim3(blocks), dim3(threads), (size_t)smem, in, P);
-        };
-        if (tn == 256) launch(splits > 1 ? affine_fp8_pair_kernel<256, true> : affine_fp8_pair_kernel<256, false>, F8Cfg<256>::kThreads, F8Cfg<256>::kSmemBytes);
-        else launch(splits > 1 ? affine_fp8_pair_kernel<128, true> : affine_fp8_pair_kernel<128, false>, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes);
+        P.splits = shape->splits;
+        const unsigned clusters = (unsigned)(shape->splits > 1 ? tiles : std::min(tiles, at_once));
+        launch_clusters_in_stream(shape->kernel, 2u * shape->splits, dim3(2u * shape->splits * clusters), dim3((unsigned)shape->threads), (size_t)shape->smem, in, P);
     }
     DISTDL_CUDA_CHECK(cudaGetLastError());
     return DISTDL_OK;

@@ -478,7 +478,10 @@ def test_adamw_beyond_32_bits_of_elements():
 # nb, features of a worker's input and output block, grid
 FP8 = [(1, 16, 16, 1, 1), (1, 128, 128, 1, 1), (2, 144, 272, 2, 3), (16, 2048, 2048, 2, 2), (17, 400, 112, 1, 2), (33, 1040, 656, 2, 2), (64, 256, 128, 4, 1),
        (65, 48, 1040, 1, 4), (100, 128, 2048, 1, 1), (128, 1296, 32, 3, 2), (129, 128, 128, 1, 1), (129, 16, 16, 2, 2), (200, 272, 656, 2, 3), (256, 2048, 256, 1, 2),
-       (256, 512, 1024, 2, 4), (300, 144, 144, 1, 1), (513, 1040, 80, 3, 1), (777, 208, 400, 2, 2), (1500, 640, 1280, 1, 1), (3000, 256, 2048, 1, 1), (1000, 4096, 96, 1, 4)]
+       (256, 512, 1024, 2, 4), (300, 144, 144, 1, 1), (513, 1040, 80, 3, 1), (777, 208, 400, 2, 2), (1500, 640, 1280, 1, 1), (3000, 256, 2048, 1, 1), (1000, 4096, 96, 1, 4),
+       # contractions of more k-blocks than a block's ring has stages, either way
+       (3, 16384, 144, 1, 1), (3, 144, 16384, 1, 1), (20, 8192, 512, 1, 2), (20, 512, 8192, 2, 1), (60, 16384, 128, 1, 1), (60, 128, 16384, 1, 1), (90, 8192, 256, 1, 2),
+       (90, 256, 8192, 2, 1), (200, 8192, 272, 1, 2), (200, 272, 8192, 2, 1), (2000, 4096, 512, 1, 1), (2000, 512, 4096, 1, 1), (1200, 5000 // 16 * 16, 1040, 1, 2)]
 
 
 def fp8_inputs(nb, bfi, bfo, pfo, pfi, adj, exact, seed=600):
