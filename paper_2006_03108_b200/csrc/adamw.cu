@@ -10,7 +10,7 @@
 namespace distdl {
 
 constexpr int kAdamThreads = 256;
-constexpr int kTileBlocks = 64;                          // blocks of 128 of a thread block's tile: 8192 elements
+constexpr int kTileBlocks = 16;                          // blocks of 128 of a thread block's tile: 2048 elements, one block each half warp
 constexpr int kTileElems = kTileBlocks * kScaleBlock;
 constexpr int kTensorsAtOnce = 320;
 
@@ -44,12 +44,18 @@ __host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// A magnitude up to 448 to an e4m3 value: floor(a / width + u) widths, width = distance of the e4m3 values at a, u in [0, 1) a multiple of 2^-16.  The
-// quotient is exact, the sum has at most the 24 bits of a float but for a carry's last one.
-__device__ __forceinline__ float stochastic_e4m3(float a, float u, bool never_zero) {
-    const uint32_t e = max(__float_as_uint(a) >> 23, 121u);                       // 2^-6 and below have one width
-    const float k = floorf(__fadd_rn(a * __uint_as_float((257u - e) << 23), u));  // 2^(3 - (e - 127))
-    return (never_zero && k == 0.f && a > 0.f ? 1.f : k) * __uint_as_float((e - 3u) << 23);
+// Code of a magnitude up to 448, rounded up or down by 16 random bits r (in bits 4 to 19): floor(a / width + r / 2^20) widths, width = distance of
+// the e4m3 values at a.  From 2^-6 on those are the numbers with three bits behind the leading one: r is added to the 20 bits behind them, a carry
+// moves on to the next value or binade, what is behind is cut off.  Below there is one width, that of 2^-6 .. 2^-5, and 2^-6 is added first.
+__device__ __forceinline__ uint32_t stochastic_e4m3(float a, uint32_t r) {
+    const bool small = a < 0x1p-6f;
+    return ((__float_as_uint(__fadd_rn(a, small ? 0x1p-6f : 0.f)) + r) >> 20) - (small ? 121u << 3 : 120u << 3);
+}
+// Root to 2^-23 or so.
+__device__ __forceinline__ float root(float v) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 struct AdamStep {
@@ -62,7 +68,7 @@ __device__ __forceinline__ void adam_element(const AdamParams &P, const AdamStep
     g *= s.grad_scale;
     m = fmaf(P.beta1, m, P.one_beta1 * g);
     v = fmaf(P.beta2, v, P.one_beta2 * g * g);
-    const float r = sqrtf(v);
+    const float r = root(v);
     p -= fmaf(s.decay, p, __fdividef(s.rate * m, fmaf(r, s.root, P.eps)));        // the weight is rounded once
     if (EIGHT) v = r;
 }
@@ -184,24 +190,23 @@ adamw_kernel(const __grid_constant__ AdamParams P) {
                 v[i] *= sv;
                 v[i] *= v[i];
                 adam_element<true>(P, s, p[i], g[i], m[i], v[i]);
-                if (element(i) >= left) m[i] = v[i] = 0.f;
+                if (!whole && element(i) >= left) m[i] = v[i] = 0.f;
                 topm = max(topm, __float_as_uint(m[i]) & 0x7fffffffu);
                 topv = max(topv, __float_as_uint(v[i]));
             }
             const BlockScale nm = block_scale(block_max(topm)), nv = block_scale(block_max(topv));
             if (lane == 0 && any) T.ms[block] = nm.scale, T.vs[block] = nv.scale;
+            // a block of 128 elements lies in one piece of 2^32
+            const uint32_t x = (uint32_t)at * 0x9E3779B9u + (uint32_t)((uint64_t)at >> 32) * 0xA54FF53Bu + s.key;
+            cm[0] = cm[1] = cv[0] = cv[1] = 0u;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint64_t e = (uint64_t)(at + element(i));
-                const uint32_t bits = mixed((uint32_t)e * 0x9E3779B9u + (uint32_t)(e >> 32) * 0xA54FF53Bu + s.key);
+                const uint32_t bits = mixed(x + (uint32_t)element(i) * 0x9E3779B9u);
                 const float a = fminf(fabsf(__fmul_rn(m[i], nm.inverse)), 448.f), b = fminf(__fmul_rn(v[i], nv.inverse), 448.f);
-                m[i] = copysignf(stochastic_e4m3(a, (float)(bits & 0xffffu) * 0x1p-16f, false), m[i]);
-                v[i] = stochastic_e4m3(b, (float)(bits >> 16) * 0x1p-16f, true);
-            }
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                cm[r] = pack_e4m3(m[4 * r], m[4 * r + 1], m[4 * r + 2], m[4 * r + 3]);
-                cv[r] = pack_e4m3(v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]);
+                const uint32_t c = stochastic_e4m3(a, (bits << 4) & 0xffff0u) | (__float_as_uint(m[i]) >> 24 & 0x80u);
+                const uint32_t d = max(stochastic_e4m3(b, (bits >> 12) & 0xffff0u), v[i] > 0.f ? 1u : 0u);
+                cm[i / 4] |= c << (i % 4 * 8);
+                cv[i / 4] |= d << (i % 4 * 8);
             }
             if (whole) {
 #pragma unroll

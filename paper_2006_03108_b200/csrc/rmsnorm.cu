@@ -454,7 +454,7 @@ struct AdjShape {
 };
 static AdjShape adj_shape(int64_t nb, int64_t chunks, bool all_bf16, int sms) {
     AdjShape a;
-    const int most = all_bf16 ? 4 : 2;
+    const int most = all_bf16 && chunks > 2 * kAdjThreads ? 4 : 2;
     a.v = chunks <= 64 ? 1 : most;
     a.group = group_of((chunks + a.v - 1) / a.v, kAdjThreads);
     a.given = chunks > (int64_t)a.v * a.group;
@@ -476,6 +476,8 @@ static void adj_launch(NormAdjParams &P, const AdjShape &a, cudaStream_t stream)
         launch_in_stream(rmsnorm_adj_kernel<T, TG, VW, kMost, true>, grid, block, 0, stream, P);
     } else if (a.v == 1) {
         launch_in_stream(rmsnorm_adj_kernel<T, TG, VW, 1, false>, grid, block, 0, stream, P);
+    } else if (a.v == 2) {
+        launch_in_stream(rmsnorm_adj_kernel<T, TG, VW, 2, false>, grid, block, 0, stream, P);
     } else {
         launch_in_stream(rmsnorm_adj_kernel<T, TG, VW, kMost, false>, grid, block, 0, stream, P);
     }
