@@ -535,7 +535,7 @@ distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_t nfo, int3
  *     never leave a code): floor(x / d + u) * d, d the distance of the codes at x, u of 16 random bits of (seed, t, tensor,
  *     element); a second moment that is not zero is held as no less than the smallest code.  All zero bits are a fresh state.
  *     The step itself uses the moments before they are rounded.
- * hyper: HOST array {lr, beta1, beta2, eps, decay, c};  step: t >= 1, the same for all tensors.
+ * hyper: HOST array {lr, beta1, beta2, eps, decay, c}, eps >= 2^-120;  step: t >= 1, the same for all tensors.
  * live: NULL, or a DEVICE array F32 {lr, t, c} that is read when the step runs and stands in the place of those three, for
  *     steps that are captured in a graph and replayed (t is exact up to 2^24).
  * count <= DISTDL_MAX_TENSORS.  One launch for every 320 tensors.  Buffers that are written may not overlap any other

@@ -44,12 +44,21 @@ __host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// Code of a magnitude up to 448, rounded up or down by 16 random bits r (in bits 4 to 19): floor(a / width + r / 2^20) widths, width = distance of
-// the e4m3 values at a.  From 2^-6 on those are the numbers with three bits behind the leading one: r is added to the 20 bits behind them, a carry
-// moves on to the next value or binade, what is behind is cut off.  Below there is one width, that of 2^-6 .. 2^-5, and 2^-6 is added first.
-__device__ __forceinline__ uint32_t stochastic_e4m3(float a, uint32_t r) {
-    const bool small = a < 0x1p-6f;
-    return ((__float_as_uint(__fadd_rn(a, small ? 0x1p-6f : 0.f)) + r) >> 20) - (small ? 121u << 3 : 120u << 3);
+// A magnitude up to 448, rounded up or down to an e4m3 value by 16 random bits: floor(a / width + u) widths, width = distance of the e4m3 values at a, u =
+// random / 2^16.  Times 2^-120, a's bits from 20 on are its code -- exponents are 120 apart, and where e4m3 numbers have one width, fp32 numbers have too --
+// and the 20 bits below are the rest, so u is added to them as bits 4 to 19 and what carries carries as it should.  The code is in bits 20 to 26
+// then; what is no number gives any code (its block's scale is none either).
+__device__ __forceinline__ uint32_t stochastic_e4m3(float a, uint32_t random16) { return __float_as_uint(fabsf(a) * 0x1p-120f) + (random16 << 4); }
+// The larger one, or NaN.
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {      // of a normal number, to 2^-23
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 // Root to 2^-23 or so.
 __device__ __forceinline__ float root(float v) {
@@ -69,7 +78,7 @@ __device__ __forceinline__ void adam_element(const AdamParams &P, const AdamStep
     m = fmaf(P.beta1, m, P.one_beta1 * g);
     v = fmaf(P.beta2, v, P.one_beta2 * g * g);
     const float r = root(v);
-    p -= fmaf(s.decay, p, __fdividef(s.rate * m, fmaf(r, s.root, P.eps)));        // the weight is rounded once
+    p -= fmaf(s.decay, p, s.rate * m * reciprocal(fmaf(r, s.root, P.eps)));       // the weight is rounded once
     if (EIGHT) v = r;
 }
 
@@ -183,7 +192,7 @@ adamw_kernel(const __grid_constant__ AdamParams P) {
             unpack_e4m3(cm[1], m + 4);
             unpack_e4m3(cv[0], v);
             unpack_e4m3(cv[1], v + 4);
-            uint32_t topm = 0, topv = 0;
+            float topm = 0.f, topv = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 m[i] *= sm;
@@ -191,22 +200,29 @@ adamw_kernel(const __grid_constant__ AdamParams P) {
                 v[i] *= v[i];
                 adam_element<true>(P, s, p[i], g[i], m[i], v[i]);
                 if (!whole && element(i) >= left) m[i] = v[i] = 0.f;
-                topm = max(topm, __float_as_uint(m[i]) & 0x7fffffffu);
-                topv = max(topv, __float_as_uint(v[i]));
+                topm = max_or_nan(topm, fabsf(m[i]));
+                topv = max_or_nan(topv, v[i]);
             }
-            const BlockScale nm = block_scale(block_max(topm)), nv = block_scale(block_max(topv));
+            const BlockScale nm = block_scale(block_max(__float_as_uint(topm) & 0x7fffffffu)), nv = block_scale(block_max(__float_as_uint(topv) & 0x7fffffffu));
             if (lane == 0 && any) T.ms[block] = nm.scale, T.vs[block] = nv.scale;
             // a block of 128 elements lies in one piece of 2^32
             const uint32_t x = (uint32_t)at * 0x9E3779B9u + (uint32_t)((uint64_t)at >> 32) * 0xA54FF53Bu + s.key;
-            cm[0] = cm[1] = cv[0] = cv[1] = 0u;
+            uint32_t c[8], d[8];                                                  // codes in the highest bytes
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t bits = mixed(x + (uint32_t)element(i) * 0x9E3779B9u);
-                const float a = fminf(fabsf(__fmul_rn(m[i], nm.inverse)), 448.f), b = fminf(__fmul_rn(v[i], nv.inverse), 448.f);
-                const uint32_t c = stochastic_e4m3(a, (bits << 4) & 0xffff0u) | (__float_as_uint(m[i]) >> 24 & 0x80u);
-                const uint32_t d = max(stochastic_e4m3(b, (bits >> 12) & 0xffff0u), v[i] > 0.f ? 1u : 0u);
-                cm[i / 4] |= c << (i % 4 * 8);
-                cv[i / 4] |= d << (i % 4 * 8);
+                uint32_t y = stochastic_e4m3(__fmul_rn(v[i], nv.inverse), bits >> 16);
+                if (v[i] > 0.f) y = max(y, 1u << 20);
+                d[i] = y << 4;
+                c[i] = (stochastic_e4m3(__fmul_rn(m[i], nm.inverse), bits & 0xffffu) << 4 & 0x7fffffffu) | (__float_as_uint(m[i]) & 0x80000000u);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const auto four = [r](const uint32_t *w) {
+                    return __byte_perm(__byte_perm(w[4 * r], w[4 * r + 1], 0x0073), __byte_perm(w[4 * r + 2], w[4 * r + 3], 0x0073), 0x5410);
+                };
+                cm[r] = four(c);
+                cv[r] = four(d) & 0x7f7f7f7fu;
             }
             if (whole) {
 #pragma unroll
@@ -256,7 +272,7 @@ static distdl_status_t adamw_impl(int32_t count, const int64_t *elems, void *con
     const double lr = hyper[0], beta1 = hyper[1], beta2 = hyper[2], eps = hyper[3], decay = hyper[4], scale = hyper[5];
     if (!rate_like(lr) || !rate_like(decay) || !std::isfinite(scale)) return fail(DISTDL_ERR_INVALID_ARG, "%s: learning rate, decay or gradient scale", what);
     if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1)) return fail(DISTDL_ERR_INVALID_ARG, "%s: betas lie in [0, 1)", what);
-    if (!std::isfinite(eps) || !((float)eps > 0)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a positive number", what);
+    if (!std::isfinite((float)eps) || !(eps >= 0x1p-120)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a number from 2^-120 on", what);
     if (step < 1 && !live) return fail(DISTDL_ERR_INVALID_ARG, "%s: steps are counted from 1", what);
     const bool eight = state == DISTDL_E4M3;
     if (count > 0 && (!p || !g || !m || !v || (eight && (!ms || !vs)))) return fail(DISTDL_ERR_INVALID_ARG, "%s: NULL argument", what);
