@@ -254,23 +254,43 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
     }
     const int64_t step = (int64_t)P.rows * groups;
     int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * groups; first < P.nb; first += step, turn ^= 1) {
-        const bool there = first + g < P.nb;
-        const int64_t row = there ? first + g : P.nb - 1;
+    struct Sample {
         Eight<TG> dy[V], dres[V];
         Eight<T> h[V];
+        float rstd, dot;
+    };
+    const auto load = [&](Sample &s, int64_t row) {
+        const bool there = row < P.nb;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int left = there ? c[v].left : 0;
             const int64_t at = row * P.bf + c[v].at;
-            dy[v].template load<VW>(reinterpret_cast<const TG *>(P.dy[c[v].worker]) + at, left);
-            h[v].template load<VW>(reinterpret_cast<const T *>(P.h[c[v].worker]) + at, left);
-            dres[v].template load<VW>(reinterpret_cast<const TG *>(P.dres[c[v].worker]) + at, P.add ? left : 0);
+            s.dy[v].template load<VW>(reinterpret_cast<const TG *>(P.dy[c[v].worker]) + at, left);
+            s.h[v].template load<VW>(reinterpret_cast<const T *>(P.h[c[v].worker]) + at, left);
+            s.dres[v].template load<VW>(reinterpret_cast<const TG *>(P.dres[c[v].worker]) + at, P.add ? left : 0);
         }
-        const float rstd = P.rstd[row];
+        s.rstd = there ? P.rstd[row] : 0.f;
+        if constexpr (GIVEN) s.dot = there ? P.dots[row] : 0.f;
+    };
+    // 16-bit values: the next sample is on its way while this one is worked on.  (32-bit ones fill the memory system by themselves, and have no registers for it.)
+    constexpr bool kAhead = sizeof(T) + sizeof(TG) <= 4 && V <= 2;
+    Sample s, next;
+    if (kAhead) load(next, (int64_t)blockIdx.x * groups + g);
+    for (int64_t first = (int64_t)blockIdx.x * groups; first < P.nb; first += step, turn ^= 1) {
+        const int64_t row = first + g;
+        const bool there = row < P.nb;
+        if (kAhead) {
+            s = next;
+            load(next, row + step);
+        } else {
+            load(s, row);
+        }
+        const auto &dy = s.dy, &dres = s.dres;
+        const auto &h = s.h;
+        const float rstd = s.rstd;
         float dot = 0.f;
         if constexpr (GIVEN) {
-            dot = P.dots[row];
+            dot = s.dot;
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) dot += norm_dot<T, TG, VW>(P, c[v], dy[v], h[v]);
@@ -325,8 +345,8 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
     }
 }
 
-// dgamma: the thread blocks' sums, eight slices of them by a warp each, the slices in order.
-constexpr int kFoldColumns = 32, kFoldSlices = 8;
+// dgamma: the thread blocks' sums, 32 slices of them by a warp each, the slices in order.
+constexpr int kFoldColumns = 32, kFoldSlices = 32;
 template <int VW>
 __global__ void __launch_bounds__(kFoldColumns * kFoldSlices)
 rmsnorm_fold_kernel(const __grid_constant__ NormAdjParams P) {
