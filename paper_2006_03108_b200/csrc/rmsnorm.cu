@@ -72,9 +72,11 @@ __device__ __forceinline__ void load_gamma(const float *g, int left, float *v) {
                 const float4 f = there ? __ldg(reinterpret_cast<const float4 *>(p + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
                 v[r * VW + i] = f.x, v[r * VW + i + 1] = f.y, v[r * VW + i + 2] = f.z, v[r * VW + i + 3] = f.w;
             }
+        } else if constexpr (VW == 2) {
+            const float2 f = there ? __ldg(reinterpret_cast<const float2 *>(p)) : make_float2(0.f, 0.f);
+            v[2 * r] = f.x, v[2 * r + 1] = f.y;
         } else {
-#pragma unroll
-            for (int i = 0; i < VW; ++i) v[r * VW + i] = there ? __ldg(p + i) : 0.f;
+            v[r] = there ? __ldg(p) : 0.f;
         }
     }
 }
@@ -202,10 +204,9 @@ struct NormAdjParams {
     bool add, params;
 };
 
-template <typename T, typename TG, int VW>
-__device__ __forceinline__ float norm_dot(const NormAdjParams &P, const ChunkAt &c, const Eight<TG> &dy, const Eight<T> &h) {
-    float g[8], dot = 0.f;
-    load_gamma<VW>(P.gamma[c.worker] + c.at, c.left, g);
+template <typename T, typename TG>
+__device__ __forceinline__ float norm_dot(const float *g, const Eight<TG> &dy, const Eight<T> &h) {
+    float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dot = fmaf(g[i] * dy.get(i), h.get(i), dot);
     return dot;
@@ -225,19 +226,22 @@ rmsnorm_dots_kernel(const __grid_constant__ NormAdjParams P) {
         Eight<T> h;
         dy.template load<VW>(reinterpret_cast<const TG *>(P.dy[c.worker]) + row * P.bf + c.at, c.left);
         h.template load<VW>(reinterpret_cast<const T *>(P.h[c.worker]) + row * P.bf + c.at, c.left);
-        dot += norm_dot<T, TG, VW>(P, c, dy, h);
+        float gamma[8];
+        load_gamma<VW>(P.gamma[c.worker] + c.at, c.left, gamma);
+        dot += norm_dot(gamma, dy, h);
     }
     dot = group_sum(dot, (int)blockDim.x, shared);
     if (threadIdx.x == 0) P.dots[row] = dot;
 }
 
-constexpr int kAdjThreads = 512;           // of a thread block at most
+// Threads of a multiprocessor by a thread's chunks: what their registers allow, and the most of a thread block
+constexpr int adj_resident(bool all_bf16, int v) { return v > 1 ? 512 : all_bf16 ? 768 : 640; }
 
 // Persistent: a thread keeps its V chunks of the features for all samples of its group (P.rows * groups apart) and sums dgamma in registers; the groups of
 // a block add up through shared memory, the blocks through `partial` and a second kernel, each in a fixed order.
 // GIVEN: the sample's sums are there already and blockIdx.y is a piece of the features.
 template <typename T, typename TG, int VW, int V, bool GIVEN>
-__global__ void __launch_bounds__(kAdjThreads, 1)
+__global__ void __launch_bounds__(adj_resident(sizeof(T) + sizeof(TG) <= 4, V), 1)
 rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
     stream_enter();
     __shared__ float shared[2][32];
@@ -245,10 +249,12 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
     const int t = threadIdx.x % P.group, g = threadIdx.x / P.group, groups = blockDim.x / P.group;
     const int chunk0 = t + blockIdx.y * P.group * V;
     ChunkAt c[V];
-    float dgamma[V][8];
+    constexpr bool kHold = V == 1;         // gamma in registers; else it comes from L1 for every sample
+    float gamma[kHold ? V : 1][8], dgamma[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         c[v] = ChunkAt::of<VW>(P, chunk0 + v * P.group);
+        if (kHold) load_gamma<VW>(P.gamma[c[v].worker] + c[v].at, c[v].left, gamma[v]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dgamma[v][i] = 0.f;
     }
@@ -272,8 +278,8 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
         s.rstd = there ? P.rstd[row] : 0.f;
         if constexpr (GIVEN) s.dot = there ? P.dots[row] : 0.f;
     };
-    // 16-bit values: the next sample is on its way while this one is worked on.  (32-bit ones fill the memory system by themselves, and have no registers for it.)
-    constexpr bool kAhead = sizeof(T) + sizeof(TG) <= 4 && V <= 2;
+    // the next sample is on its way while this one is worked on, where there are registers for it
+    constexpr bool kAhead = V == 1 || (sizeof(T) + sizeof(TG) <= 4 && V == 2);
     Sample s, next;
     if (kAhead) load(next, (int64_t)blockIdx.x * groups + g);
     for (int64_t first = (int64_t)blockIdx.x * groups; first < P.nb; first += step, turn ^= 1) {
@@ -293,18 +299,21 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
             dot = s.dot;
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) dot += norm_dot<T, TG, VW>(P, c[v], dy[v], h[v]);
+            for (int v = 0; v < V; ++v) {
+                if (!kHold) load_gamma<VW>(P.gamma[c[v].worker] + c[v].at, c[v].left, gamma[0]);
+                dot += norm_dot(gamma[kHold ? v : 0], dy[v], h[v]);
+            }
             dot = group_sum(dot, P.group, shared[turn]);
         }
         const float back = rstd * rstd * (dot * rstd / (float)P.nf);          // hhat * mean(gamma dy hhat) * rstd = h * back
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float o[8];
-            load_gamma<VW>(P.gamma[c[v].worker] + c[v].at, c[v].left, o);
+            if (!kHold) load_gamma<VW>(P.gamma[c[v].worker] + c[v].at, c[v].left, gamma[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = dy[v].get(i), x = h[v].get(i);
-                o[i] = fmaf(rstd, o[i] * d, dres[v].get(i)) - x * back;
+                o[i] = fmaf(rstd, gamma[kHold ? v : 0][i] * d, dres[v].get(i)) - x * back;
                 dgamma[v][i] = fmaf(d, x * rstd, dgamma[v][i]);
             }
             Eight<TG> e;
@@ -474,14 +483,14 @@ struct AdjShape {
 };
 static AdjShape adj_shape(int64_t nb, int64_t chunks, bool all_bf16, int sms) {
     AdjShape a;
-    const int most = all_bf16 && chunks > 2 * kAdjThreads ? 4 : 2;
-    a.v = chunks <= 64 ? 1 : most;
-    a.group = group_of((chunks + a.v - 1) / a.v, kAdjThreads);
+    // one chunk where a multiprocessor has two thread blocks of them (16 bits) or holds a sample and the next one (32 bits)
+    a.v = chunks <= (all_bf16 ? 384 : 640) ? 1 : all_bf16 && chunks > 2 * adj_resident(true, 2) ? 4 : 2;
+    a.group = group_of((chunks + a.v - 1) / a.v, adj_resident(all_bf16, a.v));
     a.given = chunks > (int64_t)a.v * a.group;
     if (a.given) a.group = 256;
     a.threads = block_of(a.group);
     a.pieces = a.given ? (int)((chunks + (int64_t)a.v * a.group - 1) / ((int64_t)a.v * a.group)) : 1;
-    const int64_t resident = (int64_t)sms * (kAdjThreads / a.threads), groups = a.threads / a.group;
+    const int64_t resident = (int64_t)sms * (adj_resident(all_bf16, a.v) / a.threads), groups = a.threads / a.group;
     a.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>((nb + groups - 1) / groups, resident / a.pieces));
     return a;
 }
