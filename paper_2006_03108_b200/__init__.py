@@ -545,16 +545,12 @@ def _float_code(what, ts):
     return code, dtype
 
 
-def _need(what, ts, n, numel, dtype):
-    """Refuses a list of blocks that is too short, and blocks of another type, size or layout than the kernels take them for (a raw
-    address says neither; the library has the last word on it)."""
-    if ts is None:
-        return
-    if len(ts) < n:
-        raise DistdlError(1, "%s is a list of %d entries, %d are needed" % (what, len(ts), n))
-    for t in ts:
-        if t.__class__ is not int and (t.dtype is not dtype or t.numel() != numel or not t.is_contiguous()):
-            raise DistdlError(2, "%s: contiguous blocks of %d elements of type %s are needed" % (what, numel, dtype))
+def _need(*lists):
+    """Refuses lists of blocks that are too short, and blocks of another type, size or layout than the kernels take them for (a raw address says
+    neither; the library has the last word on it).  Five arguments for each list: it, its entries, their elements, their type, its name."""
+    wrong = (_calls or _load()).check(*lists)
+    if wrong is not None:
+        raise DistdlError(*wrong)
 
 
 def _features(what, n, workers):
@@ -572,10 +568,9 @@ def quantize_rows(nb, nf, pf, x, q, s, stream=None):
     [ceil((nf/pf)/128), nb]."""
     code, dtype = _float_code("x", x)
     bf = _features("quantize_rows", nf, pf)
-    _need("x", x, pf, nb * bf, dtype)
-    _need("q", q, pf, nb * bf, _types["e4m3"])
-    _need("s", s, pf, nb * _blocks128(bf), _types["f32"])
-    _check((_calls or _load()).quantize_rows(nb, nf, pf, x, code, q, s, stream, pf, pf, pf))
+    n = nb * bf
+    _need(x, pf, n, dtype, "x", q, pf, n, _types["e4m3"], "q", s, pf, nb * _blocks128(bf), _types["f32"], "s")
+    _check(_calls.quantize_rows(nb, nf, pf, x, code, q, s, stream, pf, pf, pf))
 
 
 def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
@@ -583,10 +578,8 @@ def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
     [ceil((nfo/pfo)/128), ceil((nfi/pfi)/128)]."""
     code, dtype = _float_code("w", w)
     bfi, bfo, n = _features("quantize_weights", nfi, pfi), _features("quantize_weights", nfo, pfo), pfo * pfi
-    _need("w", w, n, bfo * bfi, dtype)
-    _need("q", q, n, bfo * bfi, _types["e4m3"])
-    _need("s", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"])
-    _check((_calls or _load()).quantize_weights(nfi, nfo, pfo, pfi, w, code, q, s, stream, n, n, n))
+    _need(w, n, bfo * bfi, dtype, "w", q, n, bfo * bfi, _types["e4m3"], "q", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"], "s")
+    _check(_calls.quantize_weights(nfi, nfo, pfo, pfi, w, code, q, s, stream, n, n, n))
 
 
 def rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, h=None, y=None, q=None, qs=None, rstd=None, stream=None):
@@ -594,17 +587,10 @@ def rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, h=None, y=None, q=None, qs=
     bits; each output may be None.  Lists of feature blocks [nb, nf/pf]; h may be the residual's own blocks."""
     code, dtype = _float_code("x", x)
     bf = _features("rmsnorm_fwd", nf, pf)
-    f32 = _types["f32"]
-    _need("x", x, pf, nb * bf, dtype)
-    _need("residual", residual, pf, nb * bf, dtype)
-    _need("gamma", gamma, pf, bf, f32)
-    _need("h", h, pf, nb * bf, dtype)
-    _need("y", y, pf, nb * bf, dtype)
-    _need("q", q, pf, nb * bf, _types["e4m3"])
-    _need("qs", qs, pf, nb * _blocks128(bf), f32)
-    if rstd is not None:
-        _need("rstd", (rstd,), 1, nb, f32)
-    _check((_calls or _load()).rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, code, h, y, q, qs, rstd, stream, pf, pf, pf, pf, pf, pf, pf))
+    n, f32 = nb * bf, _types["f32"]
+    _need(x, pf, n, dtype, "x", residual, pf, n, dtype, "residual", gamma, pf, bf, f32, "gamma", h, pf, n, dtype, "h", y, pf, n, dtype, "y",
+          q, pf, n, _types["e4m3"], "q", qs, pf, nb * _blocks128(bf), f32, "qs", None if rstd is None else (rstd,), 1, nb, f32, "rstd")
+    _check(_calls.rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, code, h, y, q, qs, rstd, stream, pf, pf, pf, pf, pf, pf, pf))
 
 
 def rmsnorm_adj_workspace(nb, nf, pf):
@@ -620,44 +606,30 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
     code, dtype = _float_code("h", h)
     gcode, gdtype = _float_code("dy", dy)
     bf = _features("rmsnorm_adj", nf, pf)
-    f32 = _types["f32"]
-    _need("dy", dy, pf, nb * bf, gdtype)
-    _need("dres", dres, pf, nb * bf, gdtype)
-    _need("h", h, pf, nb * bf, dtype)
-    _need("gamma", gamma, pf, bf, f32)
-    _need("rstd", (rstd,), 1, nb, f32)
-    _need("dh", dh, pf, nb * bf, gdtype)
-    _need("dgamma", dgamma, pf, bf, f32)
-    _check((_calls or _load()).rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
+    n, f32 = nb * bf, _types["f32"]
+    _need(dy, pf, n, gdtype, "dy", dres, pf, n, gdtype, "dres", h, pf, n, dtype, "h", gamma, pf, bf, f32, "gamma", (rstd,), 1, nb, f32, "rstd",
+          dh, pf, n, gdtype, "dh", dgamma, pf, bf, f32, "dgamma")
+    _check(_calls.rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
                                            workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
-
-
-def _need_fp8(what, nb, nfi, nfo, pfo, pfi, act, scales, nact, blk, w, ws, out, nout, blk_out, dtype):
-    e4m3, f32 = _types["e4m3"], _types["f32"]
-    bfi, bfo = nfi // pfi, nfo // pfo
-    _need(what[0], act, nact, nb * blk, e4m3)
-    _need(what[1], scales, nact, nb * _blocks128(blk), f32)
-    _need("w", w, pfo * pfi, bfo * bfi, e4m3)
-    _need("ws", ws, pfo * pfi, _blocks128(bfo) * _blocks128(bfi), f32)
-    _need(what[2], out, nout, nb * blk_out, dtype)
 
 
 def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
     """y_i = sum over j of x_j W_ij^T (+ bias_i) with x, xs as quantize_rows and w, ws as quantize_weights leave them; y float32 or bfloat16."""
     code, dtype = _float_code("y", y)
     bfi, bfo = _features("affine_fp8_fwd", nfi, pfi), _features("affine_fp8_fwd", nfo, pfo)
-    _need_fp8(("x", "xs", "y"), nb, nfi, nfo, pfo, pfi, x, xs, pfi, bfi, w, ws, y, pfo, bfo, dtype)
-    if bias is not None:
-        _need("bias", [b for b in bias if b is not None], 0, bfo, _types["f32"])
-    _check((_calls or _load()).affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, code, y, stream, pfi, pfi, pfo * pfi, pfo * pfi, pfo, pfo))
+    ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
+    _need(x, pfi, nb * bfi, e4m3, "x", xs, pfi, nb * ki, f32, "xs", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", y, pfo, nb * bfo, dtype, "y",
+          None if bias is None else [b for b in bias if b is not None], 0, bfo, f32, "bias")
+    _check(_calls.affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, code, y, stream, pfi, pfi, pfo * pfi, pfo * pfi, pfo, pfo))
 
 
 def affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, dx, stream=None):
     """dx_j = sum over i of dy_i W_ij with dy, dys as quantize_rows and w, ws as quantize_weights leave them; dx float32 or bfloat16."""
     code, dtype = _float_code("dx", dx)
     bfi, bfo = _features("affine_fp8_adj", nfi, pfi), _features("affine_fp8_adj", nfo, pfo)
-    _need_fp8(("dy", "dys", "dx"), nb, nfi, nfo, pfo, pfi, dy, dys, pfo, bfo, w, ws, dx, pfi, bfi, dtype)
-    _check((_calls or _load()).affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, code, dx, stream, pfo, pfo, pfo * pfi, pfo * pfi, pfi))
+    ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
+    _need(dy, pfo, nb * bfo, e4m3, "dy", dys, pfo, nb * ko, f32, "dys", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", dx, pfi, nb * bfi, dtype, "dx")
+    _check(_calls.affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, code, dx, stream, pfo, pfo, pfo * pfi, pfo * pfi, pfi))
 
 
 class AdamW:
@@ -717,7 +689,7 @@ class AdamW:
             if t.dtype is not dtype or t.numel() != k or not t.is_contiguous() or t.device != device:
                 raise DistdlError(2, "AdamW: g: contiguous tensors of the weights' sizes and device, of one type, are needed")
         if live is not None:
-            _need("live", (live,), 1, 3, _types["f32"])
+            _need((live,), 1, 3, _types["f32"], "live")
         ns = n if self._ms else 0
         _check(_calls.adamw_step(n, self._bytes, self._p, g, code, self._m, self._v, self._ms, self._vs, self._state, self._copies,
                                  (lr, betas[0], betas[1], eps, weight_decay, grad_scale), step, seed, live, stream, n, n, n, n, ns, ns,

@@ -452,7 +452,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
 // ------------------------------------------------------------------------------------------
 // Few samples (a batch of at most 128): the weights are the M operand, 128 output features a block, the batch takes N = 16, 32, 64 or 128 columns.  A
 // cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds
-// it is the stream of the weights: two blocks an SM (one for N = 128) keep it going, and its first copies leave before anything else is set up.
+// it is the stream of the weights: two blocks an SM (one from N = 64 on, whose sums need the registers of two) keep it going, and its first copies leave before anything else is set up.
 // ------------------------------------------------------------------------------------------
 constexpr int kF8WBytes = 128 * kF8K;
 constexpr int kF8FewMaxStages = 12;
@@ -464,11 +464,11 @@ struct AffineF8FewParams {
 };
 template <int N>
 struct F8FewCfg {
-    static constexpr int kParts = N >= 128 ? 2 : 1;         // summing warps: four for each part of the columns
+    static constexpr int kParts = N >= 64 ? 2 : 1;          // summing warps: four for each part of the columns
     static constexpr int kCols = N / kParts;
     static constexpr int kThreads = 128 + 128 * kParts;     // warp 0: TMA, 1: MMA and tensor memory, 3: MMA, 4..: sums
-    static constexpr int kBlocksPerSm = N >= 128 ? 1 : 2;
-    static constexpr int kLoad = N == 32 ? 32 : N >= 128 ? 64 : 16;         // columns that a tensor-memory load takes: what registers allow
+    static constexpr int kBlocksPerSm = N >= 64 ? 1 : 2;
+    static constexpr int kLoad = kCols;                     // columns that a tensor-memory load takes
     static constexpr int kStageBytes = kF8WBytes + N * kF8K;
     static constexpr int kBuffers = N >= 128 ? 2 : 4;       // products in tensor memory
     static constexpr int kTmemCols = kBuffers * N;

@@ -18,7 +18,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_cuda_stream;                 // attribute names
+PyObject *g_data_ptr, *g_cuda_stream, *g_dtype, *g_numel, *g_is_contiguous;      // attribute names
 PyObject *g_device, *g_raw_stream;                    // PyTorch's current device, and the handle of a device's current stream
 
 bool pointer_of(PyObject *number, void **out) {       // takes the reference
@@ -220,6 +220,44 @@ PyObject *taps(PyObject *, PyObject *w) {
     return Py_BuildValue("y#n", (const char *)v.data(), (Py_ssize_t)(v.size() * sizeof(float)), width / 2);
 }
 
+// check(list, n, numel, dtype, name, ...): whether every list has n entries and every tensor in it the number of elements, the type and rows without gaps
+// that the kernels take it for.  None, or (status, message) of the first that has not.  A raw address says nothing of itself, and a list may be None.
+PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n % 5) return PyErr_Format(PyExc_TypeError, "%zd arguments, a multiple of five needed", n);
+    for (; n; n -= 5, args += 5) {
+        if (args[0] == Py_None) continue;
+        const Py_ssize_t need = PyLong_AsSsize_t(args[1]);
+        const long long numel = PyLong_AsLongLong(args[2]);
+        if (PyErr_Occurred()) return nullptr;
+        PyObject *s = PySequence_Fast(args[0], "a sequence of blocks is needed");
+        if (!s) return nullptr;
+        PyObject *wrong = nullptr;
+        if (PySequence_Fast_GET_SIZE(s) < need)
+            wrong = Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S is a list of %zd entries, %zd are needed", args[4], PySequence_Fast_GET_SIZE(s), need));
+        for (Py_ssize_t i = 0; !wrong && i < PySequence_Fast_GET_SIZE(s); ++i) {
+            PyObject *t = Py_NewRef(PySequence_Fast_GET_ITEM(s, i));
+            if (!PyLong_CheckExact(t)) {
+                PyObject *dtype = PyObject_GetAttr(t, g_dtype), *count = dtype ? PyObject_CallMethodNoArgs(t, g_numel) : nullptr;
+                PyObject *whole = count ? PyObject_CallMethodNoArgs(t, g_is_contiguous) : nullptr;
+                if (whole && (dtype != args[3] || whole != Py_True || PyLong_AsLongLong(count) != numel) && !PyErr_Occurred())
+                    wrong = Py_BuildValue("iN", 2, PyUnicode_FromFormat("%S[%zd]: contiguous blocks of %lld elements of type %S are needed", args[4], i, numel, args[3]));
+                Py_XDECREF(dtype);
+                Py_XDECREF(count);
+                Py_XDECREF(whole);
+                if (PyErr_Occurred()) {
+                    Py_DECREF(t);
+                    Py_DECREF(s);
+                    return nullptr;
+                }
+            }
+            Py_DECREF(t);
+        }
+        Py_DECREF(s);
+        if (wrong || PyErr_Occurred()) return wrong;
+    }
+    Py_RETURN_NONE;
+}
+
 PyObject *set_stream_lookup(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != 2) return PyErr_Format(PyExc_TypeError, "two functions are needed");
     Py_XSETREF(g_device, Py_NewRef(args[0]));
@@ -237,6 +275,7 @@ PyMethodDef methods[] = {
     FUNCTION(quantize_rows), FUNCTION(quantize_weights), FUNCTION(rmsnorm_fwd), FUNCTION(rmsnorm_adj), FUNCTION(adamw_step),
     FUNCTION(affine_fp8_fwd), FUNCTION(affine_fp8_adj),
     {"taps", taps, METH_O, nullptr},
+    {"check", (PyCFunction)(void (*)(void))check, METH_FASTCALL, nullptr},
     {"set_stream_lookup", (PyCFunction)(void (*)(void))set_stream_lookup, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -248,6 +287,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__binding(void) {
     g_data_ptr = PyUnicode_InternFromString("data_ptr");
     g_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    g_dtype = PyUnicode_InternFromString("dtype");
+    g_numel = PyUnicode_InternFromString("numel");
+    g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     g_device = Py_NewRef(Py_None);
     g_raw_stream = Py_NewRef(Py_None);
     return PyModule_Create(&module);
