@@ -73,17 +73,22 @@ __device__ __forceinline__ void unpack_e4m3(uint32_t codes, float *v) {      // 
     }
 }
 
-// Accesses of B bytes to global memory.  Loads are coherent (a buffer may be worked on in place) and pass L1 by: every byte is read once.
+// Accesses of B bytes to global memory.  Loads are coherent (a buffer may be worked on in place).  Wide ones pass L1 by, since every byte is read once; rows
+// that are no whole number of wide ones are read in pieces that share sectors of 32 bytes, which L1 keeps for the next piece.
+// What is not there is 0, by a predicate on the load itself: a branch around narrow ones would wait for each.
 template <int B>
-__device__ __forceinline__ void ld_bytes(const void *p, uint32_t *v) {
-    if constexpr (B == 16) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "l"(p) : "memory");
-    else if constexpr (B == 8) asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "l"(p) : "memory");
-    else if constexpr (B == 4) asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v[0]) : "l"(p) : "memory");
-    else {
-        uint16_t h;
-        asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=h"(h) : "l"(p) : "memory");
-        v[0] = h;
-    }
+__device__ __forceinline__ void ld_bytes(const void *p, uint32_t *v, bool there = true) {
+    const uint32_t t = there;
+    if constexpr (B == 16)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %5, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\nmov.b32 %2, 0;\nmov.b32 %3, 0;\n@p ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n}"
+                     : "=&r"(v[0]), "=&r"(v[1]), "=&r"(v[2]), "=&r"(v[3]) : "l"(p), "r"(t) : "memory");
+    else if constexpr (B == 8)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n@p ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];\n}"
+                     : "=&r"(v[0]), "=&r"(v[1]) : "l"(p), "r"(t) : "memory");
+    else if constexpr (B == 4)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.u32 %0, [%1];\n}" : "=&r"(v[0]) : "l"(p), "r"(t) : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.u16 %0, [%1];\n}" : "=&r"(v[0]) : "l"(p), "r"(t) : "memory");
 }
 template <int B>
 __device__ __forceinline__ void st_bytes(void *p, const uint32_t *v) {
@@ -117,18 +122,16 @@ struct Eight {
     // p: the block's first element of this lane; left: elements of the row from there on (none: 0 or less).  What is not there is 0.
     template <int VW>
     __device__ __forceinline__ void load(const T *p, int left) {
+        if constexpr (VW == 1 && kHalf) {
+            uint32_t v[8];
 #pragma unroll
-        for (int r = 0; r < 8 / VW; ++r) {
-            uint32_t v[4] = {0u, 0u, 0u, 0u};
-            if (r * kBlockLanes * VW < left) ld_bytes<VW * (int)sizeof(T)>(p + r * kBlockLanes * VW, v);
-            if constexpr (VW == 1 && kHalf) {
-                if (r & 1) w[r >> 1] |= v[0] << 16;
-                else w[r >> 1] = v[0];
-            } else {
-                constexpr int words = VW * (int)sizeof(T) / 4 > 0 ? VW * (int)sizeof(T) / 4 : 1;
+            for (int r = 0; r < 8; ++r) ld_bytes<2>(p + r * kBlockLanes, v + r, r * kBlockLanes < left);
 #pragma unroll
-                for (int i = 0; i < words; ++i) w[r * words + i] = v[i];
-            }
+            for (int r = 0; r < 4; ++r) w[r] = v[2 * r] | v[2 * r + 1] << 16;
+        } else {
+            constexpr int words = VW * (int)sizeof(T) / 4;
+#pragma unroll
+            for (int r = 0; r < 8 / VW; ++r) ld_bytes<VW * (int)sizeof(T)>(p + r * kBlockLanes * VW, w + r * words, r * kBlockLanes * VW < left);
         }
     }
     template <int VW>

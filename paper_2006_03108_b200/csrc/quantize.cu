@@ -83,16 +83,8 @@ quantize_weights_kernel(const __grid_constant__ QuantWeightsParams P) {
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int u = 0; u < kRuns; ++u) {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) raw[r][u][i] = 0u;
-            if (row0 + r < P.rows && col0 + u * 32 * VW < P.cols) {
-                uint32_t v[4];
-                ld_bytes<VW * (int)sizeof(T)>(w + (int64_t)(row0 + r) * P.cols + col0 + u * 32 * VW, v);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) raw[r][u][i] = v[i];
-            }
-        }
+        for (int u = 0; u < kRuns; ++u)
+            ld_bytes<VW * (int)sizeof(T)>(w + (int64_t)(row0 + r) * P.cols + col0 + u * 32 * VW, raw[r][u], row0 + r < P.rows && col0 + u * 32 * VW < P.cols);
     const auto value = [&](int r, int u, int i) {
         if constexpr (sizeof(T) == 4) return __uint_as_float(raw[r][u][i]);
         else return __uint_as_float(i & 1 ? raw[r][u][i >> 1] & 0xffff0000u : raw[r][u][i >> 1] << 16);
