@@ -409,8 +409,8 @@ static int block_of(int group) { return group > 32 ? group : 128; }
 
 template <typename T, int VW>
 static void norm_launch(NormParams &P, cudaStream_t stream, int sms) {
-    // chunks of a thread: four of 16 bytes (two of 32) where the samples fill the device, else as few as a block of 1024 threads allows
-    constexpr int kMost = sizeof(T) == 2 ? 4 : 2;
+    // chunks of a thread: four of 16 bytes (two of 32, or of narrower pieces) where the samples fill the device, else as few as a block of 1024 threads allows
+    constexpr int kMost = sizeof(T) == 2 && VW == 8 ? 4 : 2;
     int v = P.nb >= 2 * sms ? kMost : 1;
     while (v < kMost && P.chunks > (int64_t)v * kNormMaxThreads) v *= 2;
     P.group = group_of((P.chunks + v - 1) / v, kNormMaxThreads);
