@@ -608,7 +608,7 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
     bf = _features("rmsnorm_adj", nf, pf)
     n, f32 = nb * bf, _types["f32"]
     _need(dy, pf, n, gdtype, "dy", dres, pf, n, gdtype, "dres", h, pf, n, dtype, "h", gamma, pf, bf, f32, "gamma", (rstd,), 1, nb, f32, "rstd",
-          dh, pf, n, gdtype, "dh", dgamma, pf, bf, f32, "dgamma")
+          dh, pf, n, gdtype, "dh", dgamma, pf, bf, f32, "dgamma", (workspace,), 1, workspace.numel(), workspace.dtype, "workspace")
     _check(_calls.rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
                                            workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
 
@@ -670,7 +670,7 @@ class AdamW:
         written.sort()
         if any(a[1] > b[0] for a, b in zip(written, written[1:])):
             raise DistdlError(1, "AdamW: tensors overlap")
-        self._keep = [ts for _, ts, _ in lists]
+        self._keep = [None if ts is None else tuple(ts) for _, ts, _ in lists]         # the tensors, whatever becomes of the lists
         self._count, self._bytes = n, struct.pack("%dq" % n, *self._elems)
         self._p, self._m, self._v, self._ms, self._vs, self._copies = [
             None if ts is None else struct.pack("%dQ" % n, *[0 if t is None else t.data_ptr() for t in ts]) for ts in self._keep]

@@ -18,7 +18,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_cuda_stream, *g_dtype, *g_numel, *g_is_contiguous;      // attribute names
+PyObject *g_data_ptr, *g_cuda_stream, *g_dtype, *g_numel, *g_is_contiguous, *g_get_device;      // attribute names
 PyObject *g_device, *g_raw_stream;                    // PyTorch's current device, and the handle of a device's current stream
 
 bool pointer_of(PyObject *number, void **out) {       // takes the reference
@@ -221,9 +221,13 @@ PyObject *taps(PyObject *, PyObject *w) {
 }
 
 // check(list, n, numel, dtype, name, ...): whether every list has n entries and every tensor in it the number of elements, the type and rows without gaps
-// that the kernels take it for.  None, or (status, message) of the first that has not.  A raw address says nothing of itself, and a list may be None.
+// that the kernels take it for, and whether their first tensors are on one device.  None, or (status, message) of the first that has not.  A raw address says
+// nothing of itself, and a list may be None.
 PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n % 5) return PyErr_Format(PyExc_TypeError, "%zd arguments, a multiple of five needed", n);
+    long device = -2;
+    PyObject *const *const lists = args;
+    const Py_ssize_t all = n;
     for (; n; n -= 5, args += 5) {
         if (args[0] == Py_None) continue;
         const Py_ssize_t need = PyLong_AsSsize_t(args[1]);
@@ -255,6 +259,23 @@ PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
         Py_DECREF(s);
         if (wrong || PyErr_Occurred()) return wrong;
     }
+    for (args = lists, n = all; n; n -= 5, args += 5) {
+        if (args[0] == Py_None || PySequence_Size(args[0]) < 1) continue;
+        PyObject *t = PySequence_GetItem(args[0], 0);
+        if (!t) return nullptr;
+        PyObject *on = PyLong_CheckExact(t) ? nullptr : PyObject_CallMethodNoArgs(t, g_get_device);
+        const bool raw = PyLong_CheckExact(t);
+        Py_DECREF(t);
+        if (raw) continue;
+        if (!on) return nullptr;
+        const long d = PyLong_AsLong(on);
+        Py_DECREF(on);
+        if (PyErr_Occurred()) return nullptr;
+        if (d < 0) return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S is no device memory", args[4]));
+        if (device == -2) device = d;
+        if (d != device) return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S is on device %ld, what comes before it on %ld", args[4], d, device));
+    }
+    if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
 
@@ -289,6 +310,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
     g_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     g_dtype = PyUnicode_InternFromString("dtype");
     g_numel = PyUnicode_InternFromString("numel");
+    g_get_device = PyUnicode_InternFromString("get_device");
     g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     g_device = Py_NewRef(Py_None);
     g_raw_stream = Py_NewRef(Py_None);

@@ -6,6 +6,7 @@
 // A sample's features are cut into chunks of eight values, sixteen chunks to a block of 128 (the blocks of a worker's last features are padded), so that
 // half a warp holds a block whatever the sizes and finds its scale by itself.
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "common.h"
@@ -433,7 +434,7 @@ static distdl_status_t rmsnorm_fwd_impl(int64_t nb, int64_t nf, int32_t pf, cons
     distdl_status_t st;
     if ((st = norm_shape(what, nb, nf, pf, &s))) return st;
     if (!float_type(t)) return fail(DISTDL_ERR_INVALID_ARG, "%s: values are F32 or BF16", what);
-    if (!eps || !(*eps > 0) || !((float)*eps > 0)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a positive number", what);
+    if (!eps || !(*eps > 0) || !((float)*eps > 0) || !std::isfinite((float)*eps)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a positive number", what);
     if (!h && !y && !q && !rstd) return fail(DISTDL_ERR_INVALID_ARG, "%s: no output", what);
     if (!q != !qs) return fail(DISTDL_ERR_INVALID_ARG, "%s: q and qs come together", what);
     if (nb == 0) return DISTDL_OK;

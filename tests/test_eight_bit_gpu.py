@@ -543,3 +543,223 @@ def test_affine_fp8_on_normal_numbers(case, adj):
             if t is torch.float32:
                 assert np.linalg.norm(f64(got) - ref) <= 1e-6 * np.linalg.norm(s)
         out.check()
+
+
+# ---------------------------------------------------------------------------------------------
+# The operators together, as a block of a network runs them
+# ---------------------------------------------------------------------------------------------
+
+class Block:
+    """Residual addition, norm and 8-bit affine layer on a worker grid: a training step.  All buffers are its own."""
+
+    def __init__(self, nb, bfi, bfo, pfo, pfi, seed, eight=True):
+        self.shape = nb, bfi * pfi, bfo * pfo, pfo, pfi
+        e = lambda *s, dtype=torch.float32: torch.empty(*s, device=DEV, dtype=dtype)  # noqa: E731
+        bf16, n = torch.bfloat16, pfo * pfi
+        ki, ko = -(-bfi // 128), -(-bfo // 128)
+        self.base = [dev(inputs.normal((nb, bfi), seed + j), bf16) for j in range(2 * pfi)]
+        self.dbase = [dev(inputs.normal((nb, bfo), seed + 20 + i, 0.1), bf16) for i in range(pfo)]
+        self.gamma = [dev(1 + inputs.normal((bfi,), seed + 30 + j, 0.1)) for j in range(pfi)]
+        self.w = [dev(inputs.normal((bfo, bfi), seed + 40 + i, 0.05)) for i in range(n)]
+        self.bias = [dev(inputs.normal((bfo,), seed + 60 + i)) for i in range(pfo)]
+        self.x = [torch.empty_like(a) for a in self.base]                # x, then the residual
+        self.dy = [torch.empty_like(a) for a in self.dbase]
+        self.h, self.y = [[e(nb, bfi, dtype=bf16) for _ in range(pfi)] for _ in range(2)]
+        self.q, self.qs, self.rstd = [e(nb, bfi, dtype=E4) for _ in range(pfi)], [e(ki, nb) for _ in range(pfi)], e(nb)
+        self.w8, self.ws = [e(bfo, bfi, dtype=E4) for _ in range(n)], [e(ko, ki) for _ in range(n)]
+        self.out = [e(nb, bfo, dtype=bf16) for _ in range(pfo)]
+        self.dq, self.dqs = [e(nb, bfo, dtype=E4) for _ in range(pfo)], [e(ko, nb) for _ in range(pfo)]
+        self.dx, self.dh = [[e(nb, bfi, dtype=bf16) for _ in range(pfi)] for _ in range(2)]
+        self.dgamma, self.dw, self.db = [e(bfi) for _ in range(pfi)], [e(bfo, bfi) for _ in range(n)], [e(bfo) for _ in range(pfo)]
+        self.ws_adj = e(distdl.rmsnorm_adj_workspace(nb, bfi * pfi, pfi), dtype=torch.uint8)
+        params = self.w + self.gamma + self.bias
+        zeros = lambda: [torch.zeros(a.numel(), device=DEV, dtype=torch.uint8).view(E4) for a in params]  # noqa: E731
+        scales = lambda: [torch.zeros(-(-a.numel() // 128), device=DEV) for a in params]  # noqa: E731
+        self.copies = [e(bfo, bfi, dtype=bf16) for _ in range(n)] + [None] * (pfi + pfo)
+        self.state = [zeros(), zeros(), scales(), scales()]
+        self.opt = distdl.AdamW(params, *self.state, self.copies)
+        self.factor = torch.ones((), device=DEV)
+        self.live = torch.tensor([1e-3, 1.0, 1.0], device=DEV)
+
+    def step(self, wait=lambda: None):
+        nb, nfi, nfo, pfo, pfi = self.shape
+        for a, b in zip(self.x + self.dy, self.base + self.dbase):       # the inputs, by kernels of another library
+            torch.mul(b, self.factor, out=a)
+        wait()
+        distdl.quantize_weights(nfi, nfo, pfo, pfi, self.w, self.w8, self.ws)
+        wait()
+        distdl.rmsnorm_fwd(nb, nfi, pfi, self.x[:pfi], self.x[pfi:], self.gamma, 1e-6, self.h, self.y, self.q, self.qs, self.rstd)
+        wait()
+        distdl.affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, self.q, self.qs, self.w8, self.ws, self.bias, self.out)
+        wait()
+        distdl.quantize_rows(nb, nfo, pfo, self.dy, self.dq, self.dqs)
+        wait()
+        distdl.affine_fp8_adj(nb, nfi, nfo, pfo, pfi, self.dq, self.dqs, self.w8, self.ws, self.dx)
+        wait()
+        distdl.rmsnorm_adj(nb, nfi, pfi, self.dx, self.dy if nfi == nfo and pfi == pfo else None, self.h, self.gamma, self.rstd, self.dh, self.dgamma, self.ws_adj)
+        wait()
+        distdl.affine_adj_params(nb, nfi, nfo, pfo, pfi, self.dy, self.y, self.dw, self.db)
+        wait()
+        self.opt.step(self.dw + self.dgamma + self.db, 0.0, 0, betas=(0.9, 0.95), seed=11, live=self.live)
+        wait()
+        return [a.clone() for a in self.out + self.dh + self.w + self.gamma + self.bias + self.copies[:len(self.w)]]
+
+
+GRID = [(70, 256, 384, 2, 2), (300, 144, 272, 1, 3), (1, 640, 128, 2, 1)]
+
+
+@pytest.mark.parametrize("case", GRID, ids=str)
+def test_block_of_all_operators_against_fp64(case):
+    """Each operator's result from what the one before it left, in fp64; rounding to bfloat16 half a step, sums as in the tests above."""
+    nb, bfi, bfo, pfo, pfi = case
+    b = Block(*case, 900)
+    w0, g0, c0 = [f64(a) for a in b.w], [f64(a) for a in b.gamma], [f64(a) for a in b.bias]
+    b.step()
+    distdl.device_status()
+    h = [f64(a) for a in b.h]
+    for j in range(pfi):
+        assert np.array_equal(h[j], rounded((f64(b.x[j]) + f64(b.x[pfi + j])).astype(np.float32), torch.bfloat16))
+    y, _ = o.rmsnorm_fwd(h, g0, 1e-6)
+    for a, want in zip(b.y, y):
+        assert (np.abs(f64(a) - want) <= 1.01 * 2.0 ** -8 * np.abs(want)).all()
+    for i in range(pfo * pfi):
+        same_quant(b.w8[i], b.ws[i], o.quantize_weights(w0[i]))
+    pairs = lambda q, s: [(f64(u), v.cpu().numpy()) for u, v in zip(q, s)]  # noqa: E731
+    act, w8, dq = pairs(b.q, b.qs), pairs(b.w8, b.ws), pairs(b.dq, b.dqs)
+    mag = lambda p: [(np.abs(u), v) for u, v in p]  # noqa: E731
+    for got, want, size in list(zip(b.out, o.affine_fp8_fwd(act, w8, pfo, pfi, c0), o.affine_fp8_fwd(mag(act), mag(w8), pfo, pfi, [np.abs(v) for v in c0]))) + \
+            list(zip(b.dx, o.affine_fp8_adj(dq, w8, pfo, pfi), o.affine_fp8_adj(mag(dq), mag(w8), pfo, pfi))):
+        e = 300 * U * size
+        assert (np.abs(f64(got) - want) <= e + 2.0 ** -8 * (np.abs(want) + e)).all()
+    for a, d in zip(b.dq, b.dy):
+        assert np.array_equal(f64(a), o.quantize_rows(f64(d).astype(np.float32))[0])
+    dh, dgamma = o.rmsnorm_adj([f64(a) for a in b.dx], None, h, g0, f64(b.rstd))
+    for a, want in zip(b.dh, dh):
+        assert (np.abs(f64(a) - want) <= 2.0 ** -8 * np.abs(want) + 1e-5 * np.abs(want).max()).all()
+    for a, want in zip(b.dgamma, dgamma):
+        assert np.abs(f64(a) - want).max() <= 1e-5 * np.abs(want).max()
+    for i in range(pfo):
+        for j in range(pfi):
+            want = f64(b.dy[i]).T @ f64(b.y[j])
+            assert np.abs(f64(b.dw[i * pfi + j]) - want).max() <= 1e-5 * np.abs(want).max()
+    zero = np.zeros(1)
+    for p, before, g in zip(b.w + b.gamma + b.bias, w0 + g0 + c0, b.dw + b.dgamma + b.db):
+        want, _, _ = o.adamw(before, f64(g), zero, zero, float(np.float32(1e-3)), 1, (0.9, 0.95), 1e-8, 0.01)
+        assert (np.abs(f64(p) - want) <= 1.01 * U * np.abs(want) + 32 * U * 1e-3 * (1 + np.abs(before))).all()
+    for c, p in zip(b.copies, b.w):
+        assert torch.equal(c, p.bfloat16())
+
+
+@pytest.mark.parametrize("case", GRID, ids=str)
+def test_block_captured_and_replayed_and_two_at_once(case):
+    """Steps one after another with a wait behind every operator; without; replayed from a graph; two blocks on two streams at once: the
+    same bits."""
+    def drive(b, go, results):
+        for t in range(1, 5):
+            b.factor.fill_(0.5 * t)
+            b.live.copy_(torch.tensor([1e-3 * t, float(t), 1.0], device=DEV))
+            results.append(go())
+
+    blocks = [Block(*case, 900 + 100 * (k % 2)) for k in range(6)]
+    torch.cuda.synchronize()
+    want = [[], []]
+    for k in range(2):
+        drive(blocks[k], lambda: blocks[k].step(torch.cuda.synchronize), want[k])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[] for _ in range(4)]
+    for k in range(2):                                                   # both streams are busy at once
+        with torch.cuda.stream(streams[k]):
+            drive(blocks[2 + k], blocks[2 + k].step, got[k])
+    torch.cuda.synchronize()
+    graphs, held = [], []
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[k]):
+            held.append(blocks[4 + k].step())
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for k in range(2):
+        def replay(k=k):
+            graphs[k].replay()
+            return [a.clone() for a in held[k]]
+        with torch.cuda.stream(streams[k]):
+            drive(blocks[4 + k], replay, got[2 + k])
+    distdl.device_status(streams[0])
+    torch.cuda.synchronize()
+    for k in range(4):
+        for a, b in zip(got[k], want[k % 2]):
+            assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(a, b)), k
+
+
+def test_affine_fp8_of_bad_numbers():
+    """A sample of infinities or NaN is NaN, a block of weights with one makes its columns NaN; everything else is what it is without."""
+    nb, bfi, bfo = 140, 272, 272
+    for rows in (nb, 20):
+        x, w = inputs.normal((rows, bfi), 1), inputs.normal((bfo, bfi), 2, 0.05)
+        outs = []
+        for bad in (False, True):
+            xb, wb = x.copy(), w.copy()
+            if bad:
+                xb[3, 200], xb[rows - 1, 0], wb[140, 10] = np.nan, np.inf, -np.inf
+            q, s, w8, ws = torch.empty(rows, bfi, device=DEV, dtype=E4), torch.empty(3, rows, device=DEV), torch.empty(bfo, bfi, device=DEV, dtype=E4), torch.empty(3, 3, device=DEV)
+            y = torch.empty(rows, bfo, device=DEV)
+            distdl.quantize_rows(rows, bfi, 1, [dev(xb)], [q], [s])
+            distdl.quantize_weights(bfi, bfo, 1, 1, [dev(wb)], [w8], [ws])
+            distdl.affine_fp8_fwd(rows, bfi, bfo, 1, 1, [q], [s], [w8], [ws], None, [y])
+            distdl.device_status()
+            outs.append(f64(y))
+        touched = np.zeros((rows, bfo), bool)
+        touched[[3, rows - 1]] = True
+        touched[:, 128:256] = True
+        assert np.isnan(outs[1][touched]).all() and np.array_equal(outs[1][~touched], outs[0][~touched]) and np.isfinite(outs[0]).all()
+
+
+def test_operators_on_more_than_2_31_elements():
+    """Offsets beyond 32 bits: the first and last samples of the largest batch of the layer, rows in front of and behind 2^31 elements of the others."""
+    if torch.cuda.get_device_properties(0).total_memory < 120 << 30:
+        pytest.skip("needs 60 GB")
+    nb, bfi, bfo = 1 << 20, 128, 2064
+    at = [slice(0, 300), slice(nb // 2, nb // 2 + 50), slice(nb - 300, nb)]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    x = torch.randn(nb, bfi, device=DEV, generator=g, dtype=torch.bfloat16)
+    w = [dev(inputs.normal((bfo, bfi), 3, 0.1))]
+    q, s = torch.empty(nb, bfi, device=DEV, dtype=E4), torch.empty(1, nb, device=DEV)
+    w8, ws = torch.empty(bfo, bfi, device=DEV, dtype=E4), torch.empty(17, 1, device=DEV)
+    y = torch.empty(nb, bfo, device=DEV, dtype=torch.bfloat16)
+    distdl.quantize_rows(nb, bfi, 1, [x], [q], [s])
+    distdl.quantize_weights(bfi, bfo, 1, 1, w, [w8], [ws])
+    distdl.affine_fp8_fwd(nb, bfi, bfo, 1, 1, [q], [s], [w8], [ws], None, [y])
+    distdl.device_status()
+    wv = (f64(w8), ws.cpu().numpy())
+    for r in at:
+        want = o.affine_fp8_fwd([(f64(q[r]), s[:, r].cpu().numpy())], [wv], 1, 1)[0]
+        assert (np.abs(f64(y[r]) - want) <= 1.01 * 2.0 ** -8 * np.abs(want) + 300 * U * np.abs(want).max()).all()
+    # the wide result: normed with itself as the residual, quantised, and back
+    gamma = [dev(1 + inputs.normal((bfo,), 4, 0.1))]
+    rstd, q2, s2 = torch.empty(nb, device=DEV), torch.empty(nb, bfo, device=DEV, dtype=E4), torch.empty(17, nb, device=DEV)
+    h = torch.empty_like(y)
+    distdl.rmsnorm_fwd(nb, bfo, 1, [y], [y], gamma, 1e-6, [h], None, [q2], [s2], rstd)
+    dx = torch.empty(nb, bfi, device=DEV)
+    distdl.affine_fp8_adj(nb, bfi, bfo, 1, 1, [q2], [s2], [w8], [ws], [dx])
+    distdl.device_status()
+    ws_adj = torch.empty(distdl.rmsnorm_adj_workspace(nb, bfo, 1), dtype=torch.uint8, device=DEV)
+    dh, dgamma = torch.empty_like(y), torch.empty(bfo, device=DEV)
+    distdl.rmsnorm_adj(nb, bfo, 1, [y], None, [h], gamma, rstd, [dh], [dgamma], ws_adj)
+    q3, s3 = torch.empty(nb, bfo, device=DEV, dtype=E4), torch.empty(17, nb, device=DEV)
+    distdl.quantize_rows(nb, bfo, 1, [dh], [q3], [s3])
+    torch.cuda.synchronize()
+    for r in at:
+        hv = f64(y[r]) * 2
+        assert np.array_equal(f64(h[r]), hv)
+        yw, rw = o.rmsnorm_fwd([hv], [f64(gamma[0])], 1e-6)
+        assert np.allclose(f64(rstd[r]), rw, rtol=1e-5)
+        v, scale = o.row_values(f64(q2[r]), s2[:, r].cpu().numpy()), np.repeat(f64(s2[:, r]).T, 128, 1)[:, :bfo]
+        assert (np.abs(v - yw[0]) <= np.maximum(2.0 ** -4 * np.abs(yw[0]), 2.0 ** -10 * scale) * 1.001 + 1e-5 * np.abs(yw[0])).all()
+        act = [(f64(q2[r]), s2[:, r].cpu().numpy())]
+        want, size = o.affine_fp8_adj(act, [wv], 1, 1)[0], o.affine_fp8_adj([(np.abs(act[0][0]), act[0][1])], [(np.abs(wv[0]), wv[1])], 1, 1)[0]
+        assert (np.abs(f64(dx[r]) - want) <= 300 * U * size).all()
+        dhw, _ = o.rmsnorm_adj([f64(y[r])], None, [hv], [f64(gamma[0])], f64(rstd[r]))
+        assert (np.abs(f64(dh[r]) - dhw[0]) <= 2.0 ** -8 * np.abs(dhw[0]) + 1e-5 * (np.abs(dhw[0]).max(1, keepdims=True) + np.abs(f64(y[r]) * f64(rstd[r])[:, None]))).all()
+        same_quant(q3[r], s3[:, r], o.quantize_rows(f64(dh[r]).astype(np.float32)))

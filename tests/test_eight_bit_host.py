@@ -128,7 +128,7 @@ def test_quantize_and_norm_refusals():
         lib.distdl_rmsnorm_fwd(nb, nf, pf, x, r, g, e, t, h, y, q, qs, rstd, None)  # noqa: E731
     assert fwd(nb=-1) == 1 and fwd(nf=0) == 1 and fwd(pf=9, nf=18) == 4 and fwd(nf=255) == 2 and fwd(nf=1 << 21) == 4 and fwd(nb=1 << 31) == 4
     assert fwd(e=None) == 1 and fwd(e=ctypes.byref(zero)) == 1 and fwd(e=ctypes.byref(ctypes.c_double(float("nan")))) == 1
-    assert fwd(e=ctypes.byref(ctypes.c_double(1e-60))) == 1
+    assert fwd(e=ctypes.byref(ctypes.c_double(1e-60))) == 1 and fwd(e=ctypes.byref(ctypes.c_double(float("inf")))) == 1
     assert fwd(t=distdl.F64) == 1 and fwd(x=None) == 1 and fwd(g=None) == 1 and fwd(q=None) == 1 and fwd(qs=None) == 1
     assert fwd(h=None, y=None, q=None, qs=None, rstd=None) == 1
     for name in ("x", "r", "g", "h", "y", "q", "qs"):
@@ -174,8 +174,7 @@ def test_python_calls_refuse_lists_types_sizes_and_layouts():
     refused(1, distdl.rmsnorm_fwd, 4, 256, 2, x, None, gamma, 1e-6, None, None, q, None)
     refused(1, distdl.rmsnorm_fwd, 4, 256, 2, x, None, gamma, -1.0, x)
     refused(2, distdl.rmsnorm_adj, 4, 256, 2, x, None, x, gamma, t(4), q, None, t(1 << 20))
-    if not torch.cuda.is_available():
-        refused(5, distdl.quantize_rows, 4, 256, 2, x, q, s)          # no device: nothing runs, and says so
+    refused(1, distdl.quantize_rows, 4, 256, 2, x, q, s)              # sizes and types fit, but this is host memory
 
 
 def test_adamw_refusals():
@@ -231,6 +230,11 @@ def test_adamw_handle_refuses_tensors_that_do_not_belong_together():
         opt.step(f(), 1e-3, 0, stream=0)
     assert e.value.status == 1
     distdl.AdamW([], [], []).step([], 1e-3, 1)
+    lists = [t(64)], [t(64)], [t(64)]
+    held = distdl.AdamW(*lists)
+    for x in lists:
+        x.clear()                                                                      # the handle holds the tensors themselves
+    assert [len(k) for k in held._keep if k is not None] == [1, 1, 1]
 
 
 def test_affine_fp8_refusals():
