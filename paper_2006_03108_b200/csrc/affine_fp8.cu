@@ -82,10 +82,20 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
 // 64 columns of tensor memory, and the wait for them.
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *v) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]),
+          "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]),
+          "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]),
+          "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]),
+          "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
         : "r"(taddr) : "memory");
 }
 // 4 bytes, or four zeros, to shared memory, and an arrival at a barrier once this thread's copies so far are there.
@@ -99,6 +109,15 @@ __device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
 // ------------------------------------------------------------------------------------------
 // Batches over 128: a pair of blocks owns a 256 x TN tile (cta_group::2, 128 rows and half of the weights' columns each); a cluster of S pairs shares the
 // k-blocks of a tile, in S runs one after the other, and adds up the S sums through distributed shared memory in that order.
+//
+// What bounds it.  The tensor cores take 600 clocks for a k-block of a 256 x 256 tile, and 32 KB for it come into each SM.  Large products run at what
+// power and L2 allow: 2048 x 8192 x 8192 in 127 us (2160 TFLOP/s; 11 TB/s from L2) in a burst, 4096 x 8192 x 8192 in 235 us, 274 us (2010 TFLOP/s at 1.48
+// GHz and 1 kW) when it goes on for seconds -- the same loop with all k-blocks added up in tensor memory, without scales, takes 218 and 250.  Small ones
+// are bound by what surrounds the k-blocks, some 5 to 8 us: 256 x 8192 x 8192 25 us, 777 x 3120 x 1312 13.5 us.  On the way (2048 x 8192 x 8192, us): an
+// arrival at the other block with release at the cluster's scope, a fence for every warp and k-block, 336; without 192; scalar sums instead of pairs put
+// together by moves 167; pairs that go on from tile to tile 152; one barrier for a product and its stage instead of two 143; eight summing warps with
+// 64-column loads instead of sixteen with 32-column ones 135; a second thread that issues products 127. Halves of tiles for the last turn cost the other
+// turns more than they gained (133).
 // ------------------------------------------------------------------------------------------
 constexpr int kF8Tail = 1024 + 512;                         // alignment, barriers
 constexpr int kF8ScaleSlots = 8;                            // k-blocks whose scales are on their way or waited for
@@ -141,6 +160,11 @@ struct F8Tile {
     }
 };
 
+// 4 values of a row.
+__device__ __forceinline__ void f8_store4(const AffineF8Params &P, int oblk, int64_t at, float4 v) {
+    if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[oblk]) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[oblk]) + at) = v;
+}
 // 16 values of a row: two 16-byte stores, or one of 32 bytes where the buffer allows it.
 __device__ __forceinline__ void f8_store(const AffineF8Params &P, int oblk, int64_t at, const float *v) {
     if (P.out_bf16) {
@@ -149,7 +173,8 @@ __device__ __forceinline__ void f8_store(const AffineF8Params &P, int oblk, int6
         for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
         uint16_t *p = reinterpret_cast<uint16_t *>(P.out[oblk]) + at;
         if (P.out_wide) {
-            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                         ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
         } else {
             st_bytes<16>(p, w);
             st_bytes<16>(p + 8, w + 4);
@@ -159,8 +184,8 @@ __device__ __forceinline__ void f8_store(const AffineF8Params &P, int oblk, int6
 #pragma unroll
         for (int i = 0; i < 16; i += 8) {
             if (P.out_wide) {
-                asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]), "f"(v[i + 4]), "f"(v[i + 5]),
-                             "f"(v[i + 6]), "f"(v[i + 7]) : "memory");
+                asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                             ::"l"(p + i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]), "f"(v[i + 4]), "f"(v[i + 5]), "f"(v[i + 6]), "f"(v[i + 7]) : "memory");
             } else {
                 *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                 *reinterpret_cast<float4 *>(p + i + 4) = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
@@ -419,13 +444,14 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     if (column >= P.blk_out || *abort_flag) continue;
                     const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column)) : make_float4(0.f, 0.f, 0.f, 0.f);
                     for (int rl = r0 + warp - 4; rl < r1; rl += 4 * C::kSumWarps) {
-                        float4 v[4];                                        // four rows in flight; S divides 32, so they are there
+                        float4 v[4];                                        // four rows in flight: a block has 32 of them at least
+                        const auto at_row = [&](int i) { return base + (uint32_t)(((rl + i * C::kSumWarps) * C::kPitch + c) * 4); };
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = ld_cluster_f4(map_to_cta(base + (uint32_t)(((rl + i * C::kSumWarps) * C::kPitch + c) * 4), prank));
+                        for (int i = 0; i < 4; ++i) v[i] = ld_cluster_f4(map_to_cta(at_row(i), prank));
                         for (int q = 1; q < splits; ++q) {
                             float4 w[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) w[i] = ld_cluster_f4(map_to_cta(base + (uint32_t)(((rl + i * C::kSumWarps) * C::kPitch + c) * 4), (uint32_t)(2 * q) + prank));
+                            for (int i = 0; i < 4; ++i) w[i] = ld_cluster_f4(map_to_cta(at_row(i), (uint32_t)(2 * q) + prank));
 #pragma unroll
                             for (int i = 0; i < 4; ++i) v[i].x += w[i].x, v[i].y += w[i].y, v[i].z += w[i].z, v[i].w += w[i].w;
                         }
@@ -435,8 +461,7 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                             if (row >= P.nb) continue;
                             v[i].x += b.x, v[i].y += b.y, v[i].z += b.z, v[i].w += b.w;
                             const int64_t at = (int64_t)row * P.blk_out + column;
-                            if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[t.oblk]) + at) = make_uint2(pack_bf16(v[i].x, v[i].y), pack_bf16(v[i].z, v[i].w));
-                            else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[t.oblk]) + at) = v[i];
+                            f8_store4(P, t.oblk, at, v[i]);
                         }
                     }
                 }
@@ -451,8 +476,10 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
 
 // ------------------------------------------------------------------------------------------
 // Few samples (a batch of at most 128): the weights are the M operand, 128 output features a block, the batch takes N = 16, 32, 64 or 128 columns.  A
-// cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds
-// it is the stream of the weights: two blocks an SM (one from N = 64 on, whose sums need the registers of two) keep it going, and its first copies leave before anything else is set up.
+// cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds it
+// is the stream of the weights: two blocks an SM (one from N = 64 on, whose sums need the registers of two) keep it going, and its first copies leave
+// before anything else is set up.  8192 x 8192 weights (B200, cold, in a graph): one sample 15.2 us -- of which the weights take 10.4 at the copy rate,
+// from 0.7 us after the start on -- 32 samples 16.5, 64 19.0, 128 22.0.
 // ------------------------------------------------------------------------------------------
 constexpr int kF8WBytes = 128 * kF8K;
 constexpr int kF8FewMaxStages = 12;
@@ -682,8 +709,7 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
                 }
                 o.x += bias.x, o.y += bias.y, o.z += bias.z, o.w += bias.w;
                 const int64_t at = (int64_t)row * P.blk_out + n0 + f;
-                if (P.out_bf16) *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out[oblk]) + at) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
-                else *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out[oblk]) + at) = o;
+                f8_store4(P, oblk, at, o);
             }
         }
     }
@@ -711,9 +737,10 @@ static bool make_map_u8(CUtensorMap *m, const void *ptr, int64_t rows, int64_t c
 }
 
 // Tiles of 256 or 128 columns, the contraction in one, two or four runs: the one with the least time by its clusters' turns.  Measured (B200, us): the
-// first tile without its k-blocks, each further one (a pair goes on while sums are written), a k-block.  The narrow tile reads a half more through L2 for the same
-// work, but fills SMs that wide ones leave idle; so do runs, which cost a meeting of their blocks (256 x 8192 x 8192: 256 columns in 1, 2, 4 runs 33.6, 24.9, 52.4;
-// 128 columns 25.4, 33.8, 63.3.  2048 x 8192 x 8192: 127, 180, 295; 151, 256, 425.  200 x 8192 x 1024: 31.4, 21.5, 16.4; 24.4, 16.0, 12.6).
+// first tile without its k-blocks, each further one (a pair goes on while sums are written), a k-block.  The narrow tile reads a half more through L2 for
+// the same work, but fills SMs that wide ones leave idle; so do runs, which cost a meeting of their blocks (256 x 8192 x 8192: 256 columns in 1, 2, 4 runs
+// 33.6, 24.9, 52.4; 128 columns 25.4, 33.8, 63.3.  2048 x 8192 x 8192: 127, 180, 295; 151, 256, 425.  200 x 8192 x 1024: 31.4, 21.5, 16.4; 24.4, 16.0,
+// 12.6).
 struct F8Shape {
     void (*kernel)(AffineF8Params);
     int tn, splits, threads, smem;
@@ -828,7 +855,8 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
             const F8Shape &s = kF8Shape[i];
             if ((s.splits > 1 && all < 4 * s.splits) || clusters_on[device][i] < 1) continue;
             const int64_t n_tiles = row_tiles * nout * ((P.blk_out + s.tn - 1) / s.tn), turns = (n_tiles + clusters_on[device][i] - 1) / clusters_on[device][i];
-            const double us = s.first + (double)turns * (double)((all + s.splits - 1) / s.splits) * s.kblock + (double)(turns - 1) * (s.splits > 1 ? s.first : s.next);
+            const double again = s.splits > 1 ? s.first : s.next;
+            const double us = s.first + (double)turns * (double)((all + s.splits - 1) / s.splits) * s.kblock + (double)(turns - 1) * again;
             if (!shape || us < best) {
                 best = us;
                 shape = &s;
@@ -859,7 +887,8 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
         P.tiles = (int32_t)tiles;
         P.splits = shape->splits;
         const unsigned clusters = (unsigned)(shape->splits > 1 ? tiles : std::min(tiles, at_once));
-        launch_clusters_in_stream(shape->kernel, 2u * shape->splits, dim3(2u * shape->splits * clusters), dim3((unsigned)shape->threads), (size_t)shape->smem, in, P);
+        const unsigned blocks = 2u * shape->splits;            // of a cluster
+        launch_clusters_in_stream(shape->kernel, blocks, dim3(blocks * clusters), dim3((unsigned)shape->threads), (size_t)shape->smem, in, P);
     }
     DISTDL_CUDA_CHECK(cudaGetLastError());
     return DISTDL_OK;

@@ -20,6 +20,8 @@ struct QuantRowsParams {
     int32_t bf, blocks;                    // features and blocks of a worker's row
 };
 
+// What bounds it: HBM, read once and written once.  B200: 8192 x 8192 bf16 36.5 us (5.6 TB/s), 4096 x 8192 fp32 28.5 (5.9); rows of 1001, which take
+// 2-byte loads and byte stores, 32.8 us for 8192 x 4004 (3.0 TB/s); 256 x 8192, in a graph, 2.7 us.
 // A thread block takes kSpan blocks side by side of rows r0, r0 + 1, ...: half a warp a block and row, kDepth rows of each in flight.  The scales of a block
 // lie row by row, so those of the thread block's rows fill whole lines in L2 before they leave.
 constexpr int kSpan = 4;
@@ -66,7 +68,9 @@ struct QuantWeightsParams {
     int32_t rows, cols;                    // of a worker's block
 };
 
-// A thread block holds a block of 128 x 128: a warp reads its rows in pieces of 32 VW values, 64 values a thread.
+// What bounds it: HBM.  B200, 8192 x 8192 on 4 x 4 workers: fp32 52.2 us (6.4 TB/s), bf16 33.8 (6.0); 2048 x 1001 on the same grid 35.5 (4.6). A thread
+// block holds a block of 128 x 128, so that its largest value is known without a second read: a warp reads its rows in pieces of 32 VW values, 64 values a
+// thread.
 template <typename T, int VW>
 __global__ void __launch_bounds__(kQuantThreads)
 quantize_weights_kernel(const __grid_constant__ QuantWeightsParams P) {

@@ -692,6 +692,26 @@ def test_block_captured_and_replayed_and_two_at_once(case):
             assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(a, b)), k
 
 
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", [(20, 256, 272, 1, 2), (300, 256, 272, 1, 2), (2000, 128, 1040, 2, 1), (1200, 4096, 528, 1, 1)], ids=str)
+def test_affine_fp8_into_blocks_on_16_byte_boundaries(case, t):
+    """Results that begin on a boundary of 16 bytes and not of 32: the same bits."""
+    nb, bfi, bfo, pfo, pfi = case
+    a, w = fp8_inputs(*case, False, False)
+    bias = [inputs.normal((bfo,), 700 + i) for i in range(pfo)]
+    off = 16 // t.itemsize
+    held = []
+
+    def odd(*shape, dtype):
+        buf = torch.full((shape[0] * shape[1] + 2 * off,), 7.0, device=DEV, dtype=dtype)
+        held.append(buf)
+        return buf[off:-off].view(*shape)
+
+    want, got = fp8_call(*case, False, a, w, bias, t, Out()), fp8_call(*case, False, a, w, bias, t, odd)
+    assert all(g.data_ptr() % 32 == 16 and torch.equal(g, x) for g, x in zip(got, want))
+    assert all((b[:off] == 7).all() and (b[-off:] == 7).all() for b in held)
+
+
 def test_affine_fp8_of_bad_numbers():
     """A sample of infinities or NaN is NaN, a block of weights with one makes its columns NaN; everything else is what it is without."""
     nb, bfi, bfo = 140, 272, 272
