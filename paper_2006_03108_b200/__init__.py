@@ -535,7 +535,11 @@ def _float_code(what, ts):
     if not _types:
         import torch
         _types.update({torch.float32: F32, torch.bfloat16: BF16})
-        _types["e4m3"], _types["f32"], _types["bf16"] = torch.float8_e4m3fn, torch.float32, torch.bfloat16
+        _types["e4m3"], _types["f32"] = torch.float8_e4m3fn, torch.float32
+        table = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+        if table is not None:                          # the codes that DLPack has for these types
+            _load()
+            _calls.dlpack(torch.Tensor, table, ((torch.float32, 2, 32), (torch.bfloat16, 4, 16), (torch.float8_e4m3fn, 10, 8), (torch.uint8, 1, 8)))
     if not len(ts):
         raise DistdlError(1, "%s is an empty list" % what)
     dtype = ts[0].dtype
@@ -684,12 +688,7 @@ class AdamW:
         if len(g) != n:
             raise DistdlError(1, "AdamW: g is a list of %d entries, %d are needed" % (len(g), n))
         code, dtype = _float_code("g", g)
-        device = self._device
-        for t, k in zip(g, self._elems):
-            if t.dtype is not dtype or t.numel() != k or not t.is_contiguous() or t.device != device:
-                raise DistdlError(2, "AdamW: g: contiguous tensors of the weights' sizes and device, of one type, are needed")
-        if live is not None:
-            _need((live,), 1, 3, _types["f32"], "live")
+        _need(self._keep[0][:1], 1, self._elems[0], _types["f32"], "p", g, n, self._bytes, dtype, "g", None if live is None else (live,), 1, 3, _types["f32"], "live")
         ns = n if self._ms else 0
         _check(_calls.adamw_step(n, self._bytes, self._p, g, code, self._m, self._v, self._ms, self._vs, self._state, self._copies,
                                  (lr, betas[0], betas[1], eps, weight_decay, grad_scale), step, seed, live, stream, n, n, n, n, ns, ns,

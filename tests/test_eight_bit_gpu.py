@@ -692,6 +692,27 @@ def test_block_captured_and_replayed_and_two_at_once(case):
             assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(a, b)), k
 
 
+def test_blocks_in_host_memory_are_refused():
+    """Wherever they stand in their lists: nothing is launched on them."""
+    x, host = [torch.ones(4, 128, device=DEV) for _ in range(2)], torch.ones(4, 128)
+    q, s = [torch.zeros(4, 128, device=DEV).to(E4) for _ in range(2)], [torch.zeros(1, 4, device=DEV) for _ in range(2)]
+    for bad in (dict(x=[x[0], host]), dict(x=[host, x[1]]), dict(q=[q[0], host.to(E4)]), dict(s=[s[0], torch.zeros(1, 4)])):
+        a = dict(dict(x=x, q=q, s=s), **bad)
+        with pytest.raises(distdl.DistdlError, match="host memory"):
+            distdl.quantize_rows(4, 256, 2, a["x"], a["q"], a["s"])
+    p, m, v = [torch.ones(130) for _ in range(3)]
+    with pytest.raises(distdl.DistdlError, match="host memory"):
+        distdl.AdamW([p], [m], [v]).step([p.clone()], 1e-3, 1)
+    p, m, v = [torch.ones(130, device=DEV) for _ in range(3)]
+    opt = distdl.AdamW([p], [m], [v])
+    with pytest.raises(distdl.DistdlError, match="host memory"):
+        opt.step([p.clone()], 1e-3, 1, live=torch.ones(3))
+    with pytest.raises(distdl.DistdlError, match="host memory"):
+        opt.step([torch.ones(130)], 1e-3, 1)
+    torch.cuda.synchronize()
+    assert all((a.float() == 0).all() for a in q + s) and (p == 1).all()
+
+
 @pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("case", [(20, 256, 272, 1, 2), (300, 256, 272, 1, 2), (2000, 128, 1040, 2, 1), (1200, 4096, 528, 1, 1)], ids=str)
 def test_affine_fp8_into_blocks_on_16_byte_boundaries(case, t):

@@ -269,3 +269,56 @@ def test_affine_fp8_refusals():
     refused(2, x, xs, [t(128, 144, dtype=e4).t()] * 2, ws, None, y)
     refused(2, x, [t(4)[:0]] * 2, w, ws, None, y)
     refused(2, x, xs, w, ws, [t(143)], y)
+
+
+class Block:
+    """What the checks ask a tensor for, on a device of its own."""
+
+    dtype = torch.float32
+
+    def __init__(self, device, n=8):
+        self.device, self.n = device, n
+
+    def get_device(self):
+        return self.device
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return True
+
+
+@pytest.mark.parametrize("devices, words", [([0, -1], "host memory"), ([0, 0, -1], "host memory"), ([-1, 0], "host memory"), ([1, 1, 0], "device 0, others on 1"),
+                                            ([0, 1, 2], "device 1, others on 0"), ([1, 1, 1], None)], ids=str)
+def test_every_block_is_checked_for_its_device(devices, words):
+    """Any block of any list, not the first alone; what is wrong with the sizes is said first."""
+    distdl._load()
+    for cut in range(len(devices) + 1):
+        a, b = [Block(d) for d in devices[:cut]], [Block(d) for d in devices[cut:]]
+        lists = (a, cut, 8, torch.float32, "a", None, 3, 8, torch.float32, "none", b, len(b), 8, torch.float32, "b")
+        got = distdl._calls.check(*lists)
+        assert got is None if words is None else got[0] == 1 and words in got[1], (cut, got)
+        got = distdl._calls.check(*lists, [Block(devices[0], 7)], 1, 8, torch.float32, "c")
+        assert got[0] == 2 and got[1].startswith("c[0]")
+
+
+def test_the_checks_agree_on_tensors_and_subclasses():
+    """Plain tensors go through DLPack's table where PyTorch has it, others are asked for their attributes: the same answers."""
+    class Other(torch.Tensor):
+        pass
+
+    f32, bf16, e4m3, u8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.uint8
+    distdl._float_code("x", [torch.zeros(1)])
+    base = torch.zeros(48)
+    blocks = [base.view(6, 8), base.view(6, 8).T, base.view(6, 8)[:, :5], base[::2], base.view(48, 1).T, base.view(6, 8)[2:3, :], base[:0].view(0, 4), torch.tensor(1.0),
+              base.to(bf16), base.to(e4m3), base.to(u8), base.half(), base.to(torch.float8_e5m2), base.bool(), base.clone().requires_grad_()]
+    for b in blocks:
+        for t in (f32, bf16, e4m3, u8, torch.float64):
+            for n in (b.numel(), b.numel() + 1):
+                got, want = [distdl._calls.check([a], 1, n, t, "a") for a in (b, b.as_subclass(Other))]
+                assert got == want and got[0] == (1 if b.dtype is t and n == b.numel() and b.is_contiguous() else 2), (b.dtype, b.shape, b.stride(), t, got, want)
+    sizes = np.array([48, 24, 1], np.int64).tobytes()
+    assert distdl._calls.check([base, base[:24], base[:1]], 3, sizes, f32, "a")[1] == "a: a block is in host memory"
+    assert distdl._calls.check([base, base[:23], base[:1]], 3, sizes, f32, "a")[1].startswith("a[1]: contiguous blocks of 24")
+    assert distdl._calls.check([base, base[:24], base[:1], base], 3, sizes, f32, "a")[0] == 1
