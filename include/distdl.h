@@ -24,7 +24,7 @@
  *   - The library allocates device memory only inside distdl_partition_create* and
  *     distdl_repartition_create (plan tables of a few KB to a few hundred KB, freed by the
  *     matching destroy call).  The calls that need scratch (the *_adj_params of the
- *     convolution layers) take it from the caller.
+ *     convolution layers, rmsnorm_adj) take it from the caller.
  */
 #ifndef DISTDL_H
 #define DISTDL_H
