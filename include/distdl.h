@@ -483,7 +483,8 @@ distdl_status_t distdl_quantize_weights(int64_t nfi, int64_t nfo, int32_t pfo, i
  *   [nb, nf/pf] of type tg (F32 or BF16); dh[j] may be dy's or dres's own buffers; gamma[j], dgamma[j] F32 [nf/pf]; dgamma
  *   may be NULL.  Sums over f and over b in fp32, in an order that depends on the shapes and the device alone: the same
  *   bits on every run.  workspace: device scratch of at least the size that rmsnorm_adj_workspace reports (at most some
- *   20 MB), overwritten by the call; calls that may run at the same time need one each.
+ *   10 MB, and 4 bytes a sample beyond 8192 features), overwritten by the call; calls that may run at the same time need one
+ *   each.
  * nf % pf == 0 (else DISTDL_ERR_SHAPE), pf <= 8, any block size up to nf = 2^20; nb = 0: nothing but dgamma = 0.
  * ---------------------------------------------------------------------- */
 distdl_status_t distdl_rmsnorm_fwd(int64_t nb, int64_t nf, int32_t pf, const void *const *x,
