@@ -550,11 +550,13 @@ def _float_code(what, ts):
 
 
 def _need(*lists):
-    """Refuses lists of blocks that are too short, and blocks of another type, size or layout than the kernels take them for (a raw address says
-    neither; the library has the last word on it).  Five arguments for each list: it, its entries, their elements, their type, its name."""
-    wrong = (_calls or _load()).check(*lists)
-    if wrong is not None:
-        raise DistdlError(*wrong)
+    """Addresses of lists of blocks, packed.  Refuses lists that are too short, and blocks of another type, size or layout than the kernels take them
+    for (a raw address says neither; the library has the last word on it).  Five arguments for each list: it, its entries, their elements, their type,
+    its name."""
+    found = (_calls or _load()).check(*lists)
+    if type(found[0]) is int:
+        raise DistdlError(*found)
+    return found
 
 
 def _features(what, n, workers):
@@ -573,7 +575,7 @@ def quantize_rows(nb, nf, pf, x, q, s, stream=None):
     code, dtype = _float_code("x", x)
     bf = _features("quantize_rows", nf, pf)
     n = nb * bf
-    _need(x, pf, n, dtype, "x", q, pf, n, _types["e4m3"], "q", s, pf, nb * _blocks128(bf), _types["f32"], "s")
+    x, q, s = _need(x, pf, n, dtype, "x", q, pf, n, _types["e4m3"], "q", s, pf, nb * _blocks128(bf), _types["f32"], "s")
     _check(_calls.quantize_rows(nb, nf, pf, x, code, q, s, stream, pf, pf, pf))
 
 
@@ -582,7 +584,7 @@ def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
     [ceil((nfo/pfo)/128), ceil((nfi/pfi)/128)]."""
     code, dtype = _float_code("w", w)
     bfi, bfo, n = _features("quantize_weights", nfi, pfi), _features("quantize_weights", nfo, pfo), pfo * pfi
-    _need(w, n, bfo * bfi, dtype, "w", q, n, bfo * bfi, _types["e4m3"], "q", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"], "s")
+    w, q, s = _need(w, n, bfo * bfi, dtype, "w", q, n, bfo * bfi, _types["e4m3"], "q", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"], "s")
     _check(_calls.quantize_weights(nfi, nfo, pfo, pfi, w, code, q, s, stream, n, n, n))
 
 
@@ -592,8 +594,9 @@ def rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, h=None, y=None, q=None, qs=
     code, dtype = _float_code("x", x)
     bf = _features("rmsnorm_fwd", nf, pf)
     n, f32 = nb * bf, _types["f32"]
-    _need(x, pf, n, dtype, "x", residual, pf, n, dtype, "residual", gamma, pf, bf, f32, "gamma", h, pf, n, dtype, "h", y, pf, n, dtype, "y",
-          q, pf, n, _types["e4m3"], "q", qs, pf, nb * _blocks128(bf), f32, "qs", None if rstd is None else (rstd,), 1, nb, f32, "rstd")
+    x, residual, gamma, h, y, q, qs, _ = _need(
+        x, pf, n, dtype, "x", residual, pf, n, dtype, "residual", gamma, pf, bf, f32, "gamma", h, pf, n, dtype, "h", y, pf, n, dtype, "y",
+        q, pf, n, _types["e4m3"], "q", qs, pf, nb * _blocks128(bf), f32, "qs", None if rstd is None else (rstd,), 1, nb, f32, "rstd")
     _check(_calls.rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, code, h, y, q, qs, rstd, stream, pf, pf, pf, pf, pf, pf, pf))
 
 
@@ -611,10 +614,11 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
     gcode, gdtype = _float_code("dy", dy)
     bf = _features("rmsnorm_adj", nf, pf)
     n, f32 = nb * bf, _types["f32"]
-    _need(dy, pf, n, gdtype, "dy", dres, pf, n, gdtype, "dres", h, pf, n, dtype, "h", gamma, pf, bf, f32, "gamma", (rstd,), 1, nb, f32, "rstd",
-          dh, pf, n, gdtype, "dh", dgamma, pf, bf, f32, "dgamma", (workspace,), 1, workspace.numel(), workspace.dtype, "workspace")
+    dy, dres, h, gamma, _, dh, dgamma, _ = _need(
+        dy, pf, n, gdtype, "dy", dres, pf, n, gdtype, "dres", h, pf, n, dtype, "h", gamma, pf, bf, f32, "gamma", (rstd,), 1, nb, f32, "rstd",
+        dh, pf, n, gdtype, "dh", dgamma, pf, bf, f32, "dgamma", (workspace,), 1, workspace.numel(), workspace.dtype, "workspace")
     _check(_calls.rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, code, gcode, dh, dgamma, workspace,
-                                           workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
+                              workspace.numel() * workspace.element_size(), stream, pf, pf, pf, pf, pf, pf))
 
 
 def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
@@ -622,8 +626,9 @@ def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
     code, dtype = _float_code("y", y)
     bfi, bfo = _features("affine_fp8_fwd", nfi, pfi), _features("affine_fp8_fwd", nfo, pfo)
     ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
-    _need(x, pfi, nb * bfi, e4m3, "x", xs, pfi, nb * ki, f32, "xs", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", y, pfo, nb * bfo, dtype, "y",
-          None if bias is None else [b for b in bias if b is not None], 0, bfo, f32, "bias")
+    x, xs, w, ws, y, _ = _need(
+        x, pfi, nb * bfi, e4m3, "x", xs, pfi, nb * ki, f32, "xs", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", y, pfo, nb * bfo, dtype, "y",
+        None if bias is None else [b for b in bias if b is not None], 0, bfo, f32, "bias")
     _check(_calls.affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, code, y, stream, pfi, pfi, pfo * pfi, pfo * pfi, pfo, pfo))
 
 
@@ -632,7 +637,8 @@ def affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, dx, stream=None):
     code, dtype = _float_code("dx", dx)
     bfi, bfo = _features("affine_fp8_adj", nfi, pfi), _features("affine_fp8_adj", nfo, pfo)
     ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
-    _need(dy, pfo, nb * bfo, e4m3, "dy", dys, pfo, nb * ko, f32, "dys", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", dx, pfi, nb * bfi, dtype, "dx")
+    dy, dys, w, ws, dx = _need(
+        dy, pfo, nb * bfo, e4m3, "dy", dys, pfo, nb * ko, f32, "dys", w, n, bfo * bfi, e4m3, "w", ws, n, ko * ki, f32, "ws", dx, pfi, nb * bfi, dtype, "dx")
     _check(_calls.affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, code, dx, stream, pfo, pfo, pfo * pfi, pfo * pfi, pfi))
 
 
@@ -688,7 +694,8 @@ class AdamW:
         if len(g) != n:
             raise DistdlError(1, "AdamW: g is a list of %d entries, %d are needed" % (len(g), n))
         code, dtype = _float_code("g", g)
-        _need(self._keep[0][:1], 1, self._elems[0], _types["f32"], "p", g, n, self._bytes, dtype, "g", None if live is None else (live,), 1, 3, _types["f32"], "live")
+        _, g, _ = _need(self._keep[0][:1], 1, self._elems[0], _types["f32"], "p", g, n, self._bytes, dtype, "g",
+                        None if live is None else (live,), 1, 3, _types["f32"], "live")
         ns = n if self._ms else 0
         _check(_calls.adamw_step(n, self._bytes, self._p, g, code, self._m, self._v, self._ms, self._vs, self._state, self._copies,
                                  (lr, betas[0], betas[1], eps, weight_decay, grad_scale), step, seed, live, stream, n, n, n, n, ns, ns,

@@ -268,6 +268,7 @@ PyObject *dlpack(PyObject *, PyObject *args) {
 }
 
 struct Block {
+    void *data;
     long long numel;
     long device;                                          // -1: host memory
     bool type_fits, whole;                                // whole: rows without gaps
@@ -280,6 +281,7 @@ bool look(PyObject *t, PyObject *dtype, Block *out) {
             if (d.dtype == dtype) type = &d;
     DlTensor v;
     if (type && g_dl->view(t, &v) == 0) {
+        out->data = static_cast<char *>(v.data) + v.byte_offset;
         out->type_fits = v.code == type->code && v.bits == type->bits && v.lanes == 1;
         out->device = v.device_type == 2 ? v.device : -1;
         out->numel = 1;
@@ -294,7 +296,12 @@ bool look(PyObject *t, PyObject *dtype, Block *out) {
     PyErr_Clear();                                        // a type that the table does not know, say
     PyObject *is = PyObject_GetAttr(t, g_dtype), *count = is ? PyObject_CallMethodNoArgs(t, g_numel) : nullptr;
     PyObject *whole = count ? PyObject_CallMethodNoArgs(t, g_is_contiguous) : nullptr, *on = whole ? PyObject_CallMethodNoArgs(t, g_get_device) : nullptr;
-    if (on) *out = {PyLong_AsLongLong(count), PyLong_AsLong(on), is == dtype, whole == Py_True};
+    if (on && address(t, &out->data)) {
+        out->numel = PyLong_AsLongLong(count);
+        out->device = PyLong_AsLong(on);
+        out->type_fits = is == dtype;
+        out->whole = whole == Py_True;
+    }
     Py_XDECREF(is);
     Py_XDECREF(count);
     Py_XDECREF(whole);
@@ -303,47 +310,62 @@ bool look(PyObject *t, PyObject *dtype, Block *out) {
 }
 
 // check(list, n, numel, dtype, name, ...): whether every list has n entries and every tensor in it the number of elements, the type and rows without gaps
-// that the kernels take it for, and whether they are all on one device.  None, or (status, message) of the first that has not.  A raw address says
-// nothing of itself, and a list may be None.  numel: a number, or one for each entry packed in bytes.
+// that the kernels take it for, and whether they are all on one device.  (status, message) of the first that has not; else the lists' addresses, packed in
+// bytes each, so that what is launched is what was checked.  A raw address says nothing of itself, and a list may be None.  numel: a number, or one for
+// each entry packed in bytes.
 PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n % 5) return PyErr_Format(PyExc_TypeError, "%zd arguments, a multiple of five needed", n);
     long device = -2, other = 0;                          // where the first tensor is, and the first one that is elsewhere (-1: in host memory)
-    PyObject *where = nullptr;                            // the name of that one's list, borrowed
-    for (; n; n -= 5, args += 5) {
+    PyObject *where = nullptr, *wrong = nullptr, *found = PyTuple_New(n / 5);      // where: the name of that one's list, borrowed
+    for (Py_ssize_t list = 0; found && !wrong && !PyErr_Occurred() && list < n / 5; ++list, args += 5) {
+        PyTuple_SET_ITEM(found, list, Py_NewRef(Py_None));
         if (args[0] == Py_None) continue;
         const Py_ssize_t need = PyLong_AsSsize_t(args[1]);
         const int64_t *sizes = PyBytes_Check(args[2]) ? reinterpret_cast<const int64_t *>(PyBytes_AS_STRING(args[2])) : nullptr;
         const Py_ssize_t most = sizes ? PyBytes_GET_SIZE(args[2]) / (Py_ssize_t)sizeof(int64_t) : PY_SSIZE_T_MAX;
         long long numel = sizes ? 0 : PyLong_AsLongLong(args[2]);
-        if (PyErr_Occurred()) return nullptr;
-        PyObject *s = PySequence_Fast(args[0], "a sequence of blocks is needed");
-        if (!s) return nullptr;
-        PyObject *wrong = nullptr;
-        bool looked = true;
-        if (PySequence_Fast_GET_SIZE(s) < need || PySequence_Fast_GET_SIZE(s) > most)
-            wrong = Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S is a list of %zd entries, %zd are needed", args[4], PySequence_Fast_GET_SIZE(s), need));
-        for (Py_ssize_t i = 0; looked && !wrong && i < std::min(PySequence_Fast_GET_SIZE(s), most); ++i) {      // another thread may change a list meanwhile
+        PyObject *s = PyErr_Occurred() ? nullptr : PySequence_Fast(args[0], "a sequence of blocks is needed");
+        if (!s) break;
+        const Py_ssize_t size = PySequence_Fast_GET_SIZE(s);
+        if (size < need || size > most) wrong = Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S is a list of %zd entries, %zd are needed", args[4], size, need));
+        PyObject *packed = wrong ? nullptr : PyBytes_FromStringAndSize(nullptr, size * (Py_ssize_t)sizeof(void *));
+        void **to = packed ? reinterpret_cast<void **>(PyBytes_AS_STRING(packed)) : nullptr;
+        for (Py_ssize_t i = 0; packed && !wrong && !PyErr_Occurred() && i < size; ++i) {
+            if (i >= PySequence_Fast_GET_SIZE(s)) {       // another thread may change a list meanwhile
+                PyErr_SetString(PyExc_RuntimeError, "a list changed its length during the call");
+                break;
+            }
             PyObject *t = Py_NewRef(PySequence_Fast_GET_ITEM(s, i));
             if (sizes) numel = sizes[i];
-            if (!PyLong_CheckExact(t)) {
-                Block b = {};
-                looked = look(t, args[3], &b);
-                if (looked && !(b.type_fits && b.whole && b.numel == numel))
+            Block b = {};
+            if (PyLong_CheckExact(t)) {
+                address(t, to + i);
+            } else if (look(t, args[3], &b)) {
+                to[i] = b.data;
+                if (!b.type_fits || !b.whole || b.numel != numel)
                     wrong = Py_BuildValue("iN", 2, PyUnicode_FromFormat("%S[%zd]: contiguous blocks of %lld elements of type %S are needed", args[4], i, numel, args[3]));
-                if (looked && !where && (b.device < 0 || (device >= 0 && b.device != device))) {
+                if (!where && (b.device < 0 || (device >= 0 && b.device != device))) {
                     where = args[4];
                     other = b.device;
                 }
-                if (looked && device < 0) device = b.device;
+                if (device < 0) device = b.device;
             }
             Py_DECREF(t);
         }
         Py_DECREF(s);
-        if (!looked || wrong || PyErr_Occurred()) return wrong;
+        if (packed) PyTuple_SetItem(found, list, packed);
     }
-    if (where && other < 0) return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S: a block is in host memory", where));
-    if (where) return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S: a block is on device %ld, others on %ld", where, other, device));
-    Py_RETURN_NONE;
+    if (!found || wrong || PyErr_Occurred()) {
+        Py_XDECREF(found);
+        if (PyErr_Occurred()) Py_CLEAR(wrong);
+        return wrong;
+    }
+    if (where) {
+        Py_DECREF(found);
+        if (other < 0) return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S: a block is in host memory", where));
+        return Py_BuildValue("iN", 1, PyUnicode_FromFormat("%S: a block is on device %ld, others on %ld", where, other, device));
+    }
+    return found;
 }
 
 PyObject *set_stream_lookup(PyObject *, PyObject *const *args, Py_ssize_t n) {

@@ -288,6 +288,9 @@ class Block:
     def is_contiguous(self):
         return True
 
+    def data_ptr(self):
+        return 1000 + self.device
+
 
 @pytest.mark.parametrize("devices, words", [([0, -1], "host memory"), ([0, 0, -1], "host memory"), ([-1, 0], "host memory"), ([1, 1, 0], "device 0, others on 1"),
                                             ([0, 1, 2], "device 1, others on 0"), ([1, 1, 1], None)], ids=str)
@@ -298,7 +301,10 @@ def test_every_block_is_checked_for_its_device(devices, words):
         a, b = [Block(d) for d in devices[:cut]], [Block(d) for d in devices[cut:]]
         lists = (a, cut, 8, torch.float32, "a", None, 3, 8, torch.float32, "none", b, len(b), 8, torch.float32, "b")
         got = distdl._calls.check(*lists)
-        assert got is None if words is None else got[0] == 1 and words in got[1], (cut, got)
+        if words is None:
+            assert [None if v is None else np.frombuffer(v, np.int64).tolist() for v in got] == [[d + 1000 for d in devices[:cut]], None, [d + 1000 for d in devices[cut:]]]
+        else:
+            assert got[0] == 1 and words in got[1], (cut, got)
         got = distdl._calls.check(*lists, [Block(devices[0], 7)], 1, 8, torch.float32, "c")
         assert got[0] == 2 and got[1].startswith("c[0]")
 
