@@ -48,7 +48,8 @@ struct AffineF8Params {
     int32_t kpw;                                            // k-blocks of a worker
     int32_t ws_k, ws_n;                                     // steps in the weights' scales: to the next k-block, the next 128 columns
     int32_t nout, tiles, splits;                            // output blocks; tiles and splits of the contraction (pairs)
-    int32_t adjoint, out_bf16, out_wide;                    // out_wide: every output block begins on a 32-byte boundary
+    int32_t adjoint, out_bf16;
+    int32_t out_wide, out_lines;                            // every output block begins on a 32-byte boundary; and is rows of whole 128 bytes of fp32
 };
 
 __device__ __forceinline__ bool f8_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
@@ -191,6 +192,40 @@ __device__ __forceinline__ void f8_store(const AffineF8Params &P, int oblk, int6
                 *reinterpret_cast<float4 *>(p + i + 4) = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
             }
         }
+    }
+}
+
+// 32 fp32 values of each lane's row, rows row0 + lane, columns from column on: four lanes exchange quarters, so that a store writes 128 bytes of each of
+// eight rows; 32 bytes of each of 32 rows keep L2 busy with four times the requests.  Where a row of the output is whole lines, and fp32 (B200, us):
+// 1024 x 512 x 16384 30.4 without, 25.6 so, 4096 x 1024 x 1024 12.5 and 11.4, 2048 x 8192 x 8192 137.5 and 134.7; rows that are no whole lines, and bfloat16
+// ones with half the bytes, lose by the exchange what they gain (777 x 3120 x 1312 14.2 and 14.4; in bfloat16 1321 x 2496 x 4704 26.6 and 27.3).
+__device__ __forceinline__ void f8_store_rows(const AffineF8Params &P, int oblk, int row0, int column, uint32_t *w) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int d = 1; d < 4; d *= 2) {
+        const bool odd = lane & d;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u & d) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t &lo = w[8 * u + i], &hi = w[8 * (u + d) + i];
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? lo : hi, d);
+                lo = odd ? got : lo;
+                hi = odd ? hi : got;
+            }
+        }
+    }
+    column += (lane & 3) * 8;
+    if (column >= P.blk_out) return;                        // whole groups of 16: blocks are multiples of that
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int row = row0 + (lane & ~3) + k;
+        if (row >= P.nb) break;
+        uint8_t *p = reinterpret_cast<uint8_t *>(P.out[oblk]) + ((int64_t)row * P.blk_out + column) * 4;
+        const uint32_t *v = w + 8 * k;
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
     }
 }
 
@@ -417,18 +452,34 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
             const float *bias = P.bias[t.oblk];
             if constexpr (!SPLIT) {
                 const int row = m0 + quarter * 32 + lane;
+                if (P.out_lines) {
 #pragma unroll
-                for (int c = 0; c < C::kCols; c += 16) {
-                    const int column = t.n0 + col + c;
-                    if (column >= P.blk_out) continue;                      // whole groups of 16: blocks are multiples of that
-                    float o[16];
+                    for (int c = 0; c < C::kCols; c += 32) {
+                        const int column = t.n0 + col + c;
+                        uint32_t w[32];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        const float2 lo = acc[(c + i) / 2], hi = acc[(c + i) / 2 + 1];
-                        o[i] = lo.x + b.x, o[i + 1] = lo.y + b.y, o[i + 2] = hi.x + b.z, o[i + 3] = hi.y + b.w;
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 b = bias && column < P.blk_out ? __ldg(reinterpret_cast<const float4 *>(bias + column + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float2 lo = acc[(c + i) / 2], hi = acc[(c + i) / 2 + 1];
+                            w[i] = __float_as_uint(lo.x + b.x), w[i + 1] = __float_as_uint(lo.y + b.y);
+                            w[i + 2] = __float_as_uint(hi.x + b.z), w[i + 3] = __float_as_uint(hi.y + b.w);
+                        }
+                        f8_store_rows(P, t.oblk, m0 + quarter * 32, column, w);
                     }
-                    if (row < P.nb) f8_store(P, t.oblk, (int64_t)row * P.blk_out + column, o);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < C::kCols; c += 16) {
+                        const int column = t.n0 + col + c;
+                        if (column >= P.blk_out) continue;                      // whole groups of 16: blocks are multiples of that
+                        float o[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias + column + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float2 lo = acc[(c + i) / 2], hi = acc[(c + i) / 2 + 1];
+                            o[i] = lo.x + b.x, o[i + 1] = lo.y + b.y, o[i + 2] = hi.x + b.z, o[i + 3] = hi.y + b.w;
+                        }
+                        if (row < P.nb) f8_store(P, t.oblk, (int64_t)row * P.blk_out + column, o);
+                    }
                 }
             } else {
                 // every product has been taken, so the ring is free: the sums as [row][column]
@@ -810,11 +861,12 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
     P.out_bf16 = t == DISTDL_BF16;
     P.nout = nout;
     P.out_wide = 1;
+    P.out_lines = t == DISTDL_F32 && P.blk_out % 32 == 0;
     for (int i = 0; i < nact; ++i) P.as[i] = (const float *)act_scales[i];
     for (int i = 0; i < grid; ++i) P.ws[i] = (const float *)ws[i];
     for (int i = 0; i < nout; ++i) {
         P.out[i] = out[i];
-        if (reinterpret_cast<uintptr_t>(out[i]) & 31u) P.out_wide = 0;
+        if (reinterpret_cast<uintptr_t>(out[i]) & 31u) P.out_wide = P.out_lines = 0;
         P.bias[i] = bias ? (const float *)bias[i] : nullptr;
     }
 

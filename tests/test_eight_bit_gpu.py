@@ -714,7 +714,7 @@ def test_blocks_in_host_memory_are_refused():
 
 
 @pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("case", [(20, 256, 272, 1, 2), (300, 256, 272, 1, 2), (2000, 128, 1040, 2, 1), (1200, 4096, 528, 1, 1)], ids=str)
+@pytest.mark.parametrize("case", [(20, 256, 272, 1, 2), (300, 256, 272, 1, 2), (2000, 128, 1040, 2, 1), (1200, 4096, 528, 1, 1), (300, 128, 288, 2, 1), (2300, 256, 1056, 1, 2)], ids=str)
 def test_affine_fp8_into_blocks_on_16_byte_boundaries(case, t):
     """Results that begin on a boundary of 16 bytes and not of 32: the same bits."""
     nb, bfi, bfo, pfo, pfi = case
