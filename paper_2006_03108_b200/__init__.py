@@ -534,12 +534,11 @@ def _float_code(what, ts):
     """(code, dtype) of the values of a list: F32 or BF16, by its first tensor."""
     if not _types:
         import torch
-        _types.update({torch.float32: F32, torch.bfloat16: BF16})
-        _types["e4m3"], _types["f32"] = torch.float8_e4m3fn, torch.float32
         table = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
         if table is not None:                          # the codes that DLPack has for these types
             _load()
             _calls.dlpack(torch.Tensor, table, ((torch.float32, 2, 32), (torch.bfloat16, 4, 16), (torch.float8_e4m3fn, 10, 8), (torch.uint8, 1, 8)))
+        _types.update({torch.float32: F32, torch.bfloat16: BF16, "e4m3": torch.float8_e4m3fn, "f32": torch.float32})      # at once: others may look
     if not len(ts):
         raise DistdlError(1, "%s is an empty list" % what)
     dtype = ts[0].dtype
