@@ -473,7 +473,7 @@ distdl_status_t distdl_quantize_weights(int64_t nfi, int64_t nfo, int32_t pfo, i
  * rmsnorm_fwd, for every sample b and feature f (feature blocks of nf/pf, the layout that affine_fwd reads):
  *     h = round_t(x + residual)   (residual == NULL: h = x);   rstd = 1 / sqrt(mean over all nf features of h^2 + eps);
  *     y = h * rstd * gamma, as y[j] rounded to t and / or as q[j], qs[j] in 8 bits (quantize_rows of the fp32 value).
- *   x[j], residual[j] [nb, nf/pf] of type t (F32 or BF16); gamma[j] F32 [nf/pf]; eps: HOST pointer to one value > 0.
+ *   x[j], residual[j] [nb, nf/pf] of type t (F32 or BF16); gamma[j] F32 [nf/pf]; eps: HOST pointer to one value >= 2^-120.
  *   Outputs, each list NULL if not wanted: h[j] (may be the residual's or x's own buffers: the sum in place), y[j] of type t,
  *   q[j] with qs[j]; rstd F32 [nb] or NULL.  y[j] may be x's buffers; no other overlap.  Sums in fp32.
  * rmsnorm_adj, with h and rstd of the forward pass:

@@ -315,7 +315,9 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
             }
             dot = group_sum(dot, P.group, shared[turn]);
         }
-        const float back = rstd * rstd * (dot * rstd / (float)P.nf);          // hhat * mean(gamma dy hhat) * rstd = h * back
+        // hhat * mean(gamma dy hhat) * rstd as a product with hhat: h times the square of rstd would be the same, but a root above 2^64 has no square in fp32,
+        // and a sample of zeros would be 0 * infinity
+        const float back = rstd * (dot * rstd / (float)P.nf);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float o[8];
@@ -323,8 +325,9 @@ rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = dy[v].get(i), x = h[v].get(i);
-                o[i] = fmaf(rstd, gamma[kHold ? v : 0][i] * d, dres[v].get(i)) - x * back;
-                dgamma[v][i] = fmaf(d, x * rstd, dgamma[v][i]);
+                const float hat = x * rstd;
+                o[i] = fmaf(rstd, gamma[kHold ? v : 0][i] * d, dres[v].get(i)) - hat * back;
+                dgamma[v][i] = fmaf(d, hat, dgamma[v][i]);
             }
             Eight<TG> e;
             e.set(o);
@@ -443,7 +446,8 @@ static distdl_status_t rmsnorm_fwd_impl(int64_t nb, int64_t nf, int32_t pf, cons
     distdl_status_t st;
     if ((st = norm_shape(what, nb, nf, pf, &s))) return st;
     if (!float_type(t)) return fail(DISTDL_ERR_INVALID_ARG, "%s: values are F32 or BF16", what);
-    if (!eps || !(*eps > 0) || !((float)*eps > 0) || !std::isfinite((float)*eps)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a positive number", what);
+    // below 2^-120 the squares of what weighs against eps are subnormal in fp32, and their sum is no longer good to its roundings
+    if (!eps || !(*eps >= 0x1p-120) || !std::isfinite((float)*eps)) return fail(DISTDL_ERR_INVALID_ARG, "%s: eps must be a number from 2^-120 on", what);
     if (!h && !y && !q && !rstd) return fail(DISTDL_ERR_INVALID_ARG, "%s: no output", what);
     if (!q != !qs) return fail(DISTDL_ERR_INVALID_ARG, "%s: q and qs come together", what);
     if (nb == 0) return DISTDL_OK;

@@ -1,0 +1,70 @@
+"""GPU tests of the operators of 8-bit affine blocks at the ends of their ranges, against the oracle (fp64); tolerances as in test_eight_bit_gpu.py."""
+
+import numpy as np
+import pytest
+
+import paper_2006_03108_b200 as distdl
+from oracle import eight_bit as o
+from paper_2006_03108_b200 import inputs
+from test_eight_bit_gpu import DEV, U, Out, dev, eps_of, f64, rounded, sum_error
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+# a chunk of a thread, two, four; sums over the features by a kernel of their own; rows of odd lengths
+NEAR_ZERO = [(24, 136, 2), (24, 40, 1), (12, 2048, 2), (12, 2500, 4), (12, 5003, 4)]
+
+
+@pytest.mark.parametrize("tg", [torch.float32, torch.bfloat16], ids=["gf32", "gbf16"])
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("nb,bf,pf", NEAR_ZERO, ids=str)
+def test_rmsnorm_adj_of_samples_near_zero(t, tg, nb, bf, pf):
+    """Samples of zeros and next to zero, whose rstd has no square in fp32: dh is the number that the formula gives, and no NaN."""
+    nf = bf * pf
+    size = np.array([0.0, 1e-30, 1e-24, 1e-21, 1e-15, 1.0] * (nb // 6))[:, None]
+    eps = np.array([1e-44, 1e-42, 1e-44, 1e-40, 2.0 ** -120, 1e-6] * (nb // 6))
+    h = [rounded((inputs.normal((nb, bf), 500 + j) * size).astype(np.float32), t) for j in range(pf)]
+    dy = [rounded(inputs.normal((nb, bf), 520 + j, 300.0), tg) for j in range(pf)]
+    dres = [rounded(inputs.normal((nb, bf), 540 + j, 0.1), tg) for j in range(pf)]
+    g = [1 + inputs.normal((bf,), 560 + j, 0.2) for j in range(pf)]
+    h64, g64, d64 = ([a.astype(np.float64) for a in v] for v in (h, g, dy))
+    rstd = (1 / np.sqrt(sum((a ** 2).sum(1) for a in h64) / nf + eps)).astype(np.float32)
+    assert (rstd.max() > 2.0 ** 64) and np.isfinite(rstd).all()
+    out = Out()
+    dh, dg = [out(nb, bf, dtype=tg) for _ in range(pf)], [out(bf) for _ in range(pf)]
+    ws = out(distdl.rmsnorm_adj_workspace(nb, nf, pf), dtype=torch.uint8)
+    distdl.rmsnorm_adj(nb, nf, pf, [dev(a, tg) for a in dy], [dev(a, tg) for a in dres], [dev(a, t) for a in h], [dev(a) for a in g], dev(rstd), dh, dg, ws)
+    dhw, dgw = o.rmsnorm_adj(d64, [a.astype(np.float64) for a in dres], h64, g64, rstd)
+    r = rstd.astype(np.float64)[:, None]
+    terms = sum((np.abs(a * b * c)).sum(1, keepdims=True) for a, b, c in zip(d64, h64, g64)) / nf
+    for j in range(pf):
+        back = np.abs(h64[j]) * r ** 3 * terms
+        e = (sum_error(nf, pf) + 8 * U) * back + 4 * U * (np.abs(r * g64[j] * d64[j]) + np.abs(dres[j]) + back)
+        assert (np.abs(f64(dh[j]) - dhw[j]) <= e + eps_of(tg) * (np.abs(dhw[j]) + e)).all()
+        assert (np.abs(f64(dg[j]) - dgw[j]) <= (28 + 4) * U * np.abs(d64[j] * h64[j] * r).sum(0)).all()
+    out.check()
+
+
+def test_rmsnorm_forward_and_back_with_the_smallest_eps():
+    """The forward pass's own rstd at the smallest eps: samples of zeros, next to it and ordinary ones."""
+    nb, bf, pf, eps = 9, 200, 2, 2.0 ** -120
+    size = np.array([0.0, 2.0 ** -62, 1.0] * 3)[:, None].astype(np.float32)
+    h, dy, g = [[inputs.normal(s, 600 + 10 * k + j) for j in range(pf)] for k, s in enumerate(((nb, bf), (nb, bf), (bf,)))]
+    h = [a * size for a in h]
+    hd, gd, rstd = [dev(a) for a in h], [dev(a) for a in g], torch.empty(nb, device=DEV)
+    y, dh, dg = [[torch.empty(*s, device=DEV) for _ in range(pf)] for s in ((nb, bf), (nb, bf), (bf,))]
+    distdl.rmsnorm_fwd(nb, bf * pf, pf, hd, None, gd, eps, None, y, None, None, rstd)
+    distdl.rmsnorm_adj(nb, bf * pf, pf, [dev(a) for a in dy], None, hd, gd, rstd, dh, dg,
+                       torch.empty(distdl.rmsnorm_adj_workspace(nb, bf * pf, pf), dtype=torch.uint8, device=DEV))
+    h64, g64, d64 = ([a.astype(np.float64) for a in v] for v in (h, g, dy))
+    yw, rw = o.rmsnorm_fwd(h64, g64, eps)
+    re = sum_error(bf * pf, pf) / 2 + 4 * U + 2.0 ** -30                       # the last: squares below 2^-126, each to 2^-150
+    assert (np.abs(f64(rstd) - rw) <= re * rw).all()
+    dhw, _ = o.rmsnorm_adj(d64, None, h64, g64, f64(rstd))
+    terms = sum((np.abs(a * b * c)).sum(1, keepdims=True) for a, b, c in zip(d64, h64, g64)) / (bf * pf)
+    r = f64(rstd)[:, None]
+    for j in range(pf):
+        assert (np.abs(f64(y[j]) - yw[j]) <= (re + 3 * U) * np.abs(yw[j]) * (1 + U)).all()
+        back = np.abs(h64[j]) * r ** 3 * terms
+        e = (sum_error(bf * pf, pf) + 8 * U) * back + 4 * U * (np.abs(r * g64[j] * d64[j]) + back)
+        assert (np.abs(f64(dh[j]) - dhw[j]) <= e + U * (np.abs(dhw[j]) + e)).all()
