@@ -647,7 +647,9 @@ class AdamW:
 
     m, v: float32, or float8_e4m3fn with scales ms, vs (float32, one for every 128 elements); zeros are a fresh state.  copies:
     bfloat16 tensors that receive the new weights, or None for some or all.  The tensors are checked and their addresses taken here:
-    they have to stay where they are (in-place operations and loads are fine) as long as the handle is used."""
+    they have to stay where they are (in-place operations and loads are fine) as long as the handle is used.  The handle holds their
+    memory; a step refuses weights or copies that have other memory since (`p.data = ...`, a module's `to()`): make a new handle then.  A
+    state that gets other memory is not looked at: the handle goes on with what it holds.  A captured step goes to what it was captured with."""
 
     def __init__(self, p, m, v, ms=None, vs=None, copies=None):
         import torch
@@ -683,6 +685,9 @@ class AdamW:
         self._count, self._bytes = n, struct.pack("%dq" % n, *self._elems)
         self._p, self._m, self._v, self._ms, self._vs, self._copies = [
             None if ts is None else struct.pack("%dQ" % n, *[0 if t is None else t.data_ptr() for t in ts]) for ts in self._keep]
+        self._memory = [t.untyped_storage() for ts in self._keep if ts is not None for t in ts if t is not None]      # stays, whatever becomes of the tensors
+        # What a program may give other memory behind the handle's back are a model's weights; each step looks at those (50 ns a tensor)
+        self._watch = [self._keep[0], self._p, "p"] + ([self._keep[5], self._copies, "copies"] if self._copies else [])
 
     def step(self, g, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, seed=0, grad_scale=1.0, live=None, stream=None):
         """One step (the step-th, from 1) with gradients g (float32 or bfloat16); seed: of the rounding of states in 8 bits; live: a
@@ -692,6 +697,9 @@ class AdamW:
             return
         if len(g) != n:
             raise DistdlError(1, "AdamW: g is a list of %d entries, %d are needed" % (len(g), n))
+        gone = _calls.moved(*self._watch)
+        if gone is not None:
+            raise DistdlError(1, "AdamW: " + gone)
         code, dtype = _float_code("g", g)
         _, g, _ = _need(self._keep[0][:1], 1, self._elems[0], _types["f32"], "p", g, n, self._bytes, dtype, "g",
                         None if live is None else (live,), 1, 3, _types["f32"], "live")

@@ -6,7 +6,7 @@ import pytest
 import paper_2006_03108_b200 as distdl
 from oracle import eight_bit as o
 from paper_2006_03108_b200 import inputs
-from test_eight_bit_gpu import DEV, U, Out, dev, eps_of, f64, rounded, sum_error
+from test_eight_bit_gpu import DEV, E4, U, Out, dev, eps_of, f64, rounded, sum_error
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -68,3 +68,25 @@ def test_rmsnorm_forward_and_back_with_the_smallest_eps():
         back = np.abs(h64[j]) * r ** 3 * terms
         e = (sum_error(bf * pf, pf) + 8 * U) * back + 4 * U * (np.abs(r * g64[j] * d64[j]) + back)
         assert (np.abs(f64(dh[j]) - dhw[j]) <= e + U * (np.abs(dhw[j]) + e)).all()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+def test_adamw_writes_nothing_once_a_tensor_has_moved(eight):
+    """A parameter that got other memory: the step is refused, and neither the old memory nor the new one changes."""
+    n = 1000
+    p = [torch.nn.Parameter(torch.ones(n, device=DEV)) for _ in range(2)]
+    state = [[torch.zeros(n, device=DEV, dtype=E4 if eight else torch.float32) for _ in range(2)] for _ in range(2)]
+    scales = [[torch.zeros(8, device=DEV) for _ in range(2)] for _ in range(2)] if eight else []
+    opt, g = distdl.AdamW(p, *state, *scales), [torch.ones(n, device=DEV) for _ in range(2)]
+    opt.step(g, 1e-3, 1)
+    before = [a.detach().clone() for a in p]
+    old = p[1].data
+    p[1].data = p[1].data.clone()
+    with pytest.raises(distdl.DistdlError, match="no longer") as e:
+        opt.step(g, 1e-3, 2)
+    assert e.value.status == 1
+    torch.cuda.synchronize()
+    assert torch.equal(p[0], before[0]) and torch.equal(p[1], before[1]) and torch.equal(old, before[1])
+    distdl.AdamW(p, *state, *scales).step(g, 1e-3, 2)
+    torch.cuda.synchronize()
+    assert not torch.equal(p[1], before[1]) and torch.equal(old, before[1])

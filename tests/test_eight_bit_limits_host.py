@@ -21,3 +21,39 @@ def test_norm_refuses_eps_whose_squares_are_subnormal():
     for eps in (2.0 ** -120 * (1 - 2.0 ** -50), 2.0 ** -121, 2.0 ** -130, 1e-45, 0.0, -1.0, float("nan"), float("inf"), 1e39):
         assert status(eps) == 1 and status(eps, 4) == 1, eps
         assert b"eps" in lib.distdl_last_error()
+
+
+def test_adamw_refuses_tensors_that_have_moved():
+    """Weights and their copies are where they were or the step says so; the memory of all tensors is held, so that no step writes to what is another's."""
+    e4 = torch.float8_e4m3fn
+    names = "p", "m", "v", "ms", "vs", "copies"
+    for k, name in enumerate(names):
+        for parameter in (False, True):
+            sizes = 300, 0, 5
+            lists = [[torch.zeros(n, dtype=t) for n in sizes] for t in (torch.float32, e4, e4)] + [[torch.zeros(-(-n // 128)) for n in sizes] for _ in range(2)]
+            lists.append([torch.zeros(300, dtype=torch.bfloat16), None, torch.zeros(5, dtype=torch.bfloat16)])
+            if parameter:
+                lists[0] = [torch.nn.Parameter(a) for a in lists[0]]
+            opt = distdl.AdamW(*lists)
+            g = [torch.zeros(n) for n in sizes]
+
+            def step(words):
+                with pytest.raises(distdl.DistdlError, match=words) as e:
+                    opt.step(g, 1e-3, 1, stream=0)
+                assert e.value.status == 1
+
+            step("host memory")                                       # where they were: on to the next check
+            with torch.no_grad():
+                lists[0][0].add_(1)
+                lists[3][2].copy_(torch.ones(1))
+            step("host memory")
+            t = lists[k][2]
+            old = t.data_ptr()
+            t.data = t.data.clone()
+            assert t.data_ptr() != old and any(m.data_ptr() == old for m in opt._memory)
+            step(name + r"\[2\] is no longer where it was" if name in ("p", "copies") else "host memory")
+            step("no longer" if name in ("p", "copies") else "host memory")
+    with pytest.raises(TypeError):
+        distdl._calls.moved((torch.zeros(1),), b"", "p")
+    with pytest.raises(TypeError):
+        distdl._calls.moved((torch.zeros(1),), b"\0" * 8)
