@@ -320,7 +320,7 @@ PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
     for (Py_ssize_t list = 0; found && !wrong && !PyErr_Occurred() && list < n / 5; ++list, args += 5) {
         PyTuple_SET_ITEM(found, list, Py_NewRef(Py_None));
         if (args[0] == Py_None) continue;
-        const Py_ssize_t need = PyLong_AsSsize_t(args[1]);
+        const Py_ssize_t need = PyNumber_AsSsize_t(args[1], PyExc_OverflowError);      // any type with __index__
         const int64_t *sizes = PyBytes_Check(args[2]) ? reinterpret_cast<const int64_t *>(PyBytes_AS_STRING(args[2])) : nullptr;
         const Py_ssize_t most = sizes ? PyBytes_GET_SIZE(args[2]) / (Py_ssize_t)sizeof(int64_t) : PY_SSIZE_T_MAX;
         long long numel = sizes ? 0 : PyLong_AsLongLong(args[2]);

@@ -2,6 +2,7 @@
 
 import ctypes
 
+import numpy as np
 import pytest
 
 import paper_2006_03108_b200 as distdl
@@ -57,3 +58,27 @@ def test_adamw_refuses_tensors_that_have_moved():
         distdl._calls.moved((torch.zeros(1),), b"", "p")
     with pytest.raises(TypeError):
         distdl._calls.moved((torch.zeros(1),), b"\0" * 8)
+
+
+@pytest.mark.parametrize("kind", [np.int64, np.int32, np.int16, np.int8, np.uint8])
+def test_whole_numbers_of_any_type(kind):
+    """NumPy's numbers are taken as Python's are: all checks pass up to the one that finds host memory, and their products do not wrap around."""
+    t = lambda *shape, dtype=torch.float32: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    e4 = torch.float8_e4m3fn
+    nb, bf, pf, e = 100, 32, 2, t(100, 32)
+    i = [kind(v) for v in (nb, bf * pf, pf)]
+    rows, q, s, gamma = [e, e], [t(nb, bf, dtype=e4)] * 2, [t(1, nb)] * 2, [t(bf)] * 2
+    w, w8, ws = [t(bf, bf)] * 4, [t(bf, bf, dtype=e4)] * 4, [t(1, 1)] * 4
+    grid = i[1], i[1], i[2], i[2]
+    calls = (lambda: distdl.quantize_rows(*i, rows, q, s, stream=0), lambda: distdl.quantize_weights(*grid, w, w8, ws, stream=0),
+             lambda: distdl.rmsnorm_fwd(*i, rows, rows, gamma, 1e-6, rows, None, q, s, t(nb), stream=0),
+             lambda: distdl.rmsnorm_adj(*i, rows, None, rows, gamma, t(nb), rows, None, t(1 << 20), stream=0),
+             lambda: distdl.affine_fp8_fwd(i[0], *grid, q, s, w8, ws, gamma, rows, stream=0), lambda: distdl.affine_fp8_adj(i[0], *grid, q, s, w8, ws, rows, stream=0))
+    for call in calls:
+        with pytest.raises(distdl.DistdlError, match="host memory") as err:
+            call()
+        assert err.value.status == 1
+    with pytest.raises(TypeError):
+        distdl.quantize_rows(4.0, 64, 2, rows, q, s, stream=0)
+    with pytest.raises(TypeError):
+        distdl.affine_fp8_fwd(nb, 64, 64, 2, "2", q, s, w8, ws, None, rows, stream=0)
