@@ -118,6 +118,10 @@ struct Pointers {                                     // shards, or their addres
     bool read(PyObject *o, bool) {
         if (o == Py_None) return true;
         if (PyBytes_Check(o)) {
+            if (PyBytes_GET_SIZE(o) % (Py_ssize_t)sizeof(void *)) {
+                PyErr_Format(PyExc_ValueError, "%zd bytes are no whole number of addresses", PyBytes_GET_SIZE(o));
+                return false;
+            }
             p = reinterpret_cast<void **>(PyBytes_AS_STRING(o));
             size = PyBytes_GET_SIZE(o) / (Py_ssize_t)sizeof(void *);
             return true;
@@ -322,6 +326,10 @@ PyObject *check(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (args[0] == Py_None) continue;
         const Py_ssize_t need = PyNumber_AsSsize_t(args[1], PyExc_OverflowError);      // any type with __index__
         const int64_t *sizes = PyBytes_Check(args[2]) ? reinterpret_cast<const int64_t *>(PyBytes_AS_STRING(args[2])) : nullptr;
+        if (sizes && PyBytes_GET_SIZE(args[2]) % (Py_ssize_t)sizeof(int64_t)) {
+            PyErr_Format(PyExc_ValueError, "%zd bytes are no whole number of sizes", PyBytes_GET_SIZE(args[2]));
+            break;
+        }
         const Py_ssize_t most = sizes ? PyBytes_GET_SIZE(args[2]) / (Py_ssize_t)sizeof(int64_t) : PY_SSIZE_T_MAX;
         long long numel = sizes ? 0 : PyLong_AsLongLong(args[2]);
         PyObject *s = PyErr_Occurred() ? nullptr : PySequence_Fast(args[0], "a sequence of blocks is needed");

@@ -82,3 +82,23 @@ def test_whole_numbers_of_any_type(kind):
         distdl.quantize_rows(4.0, 64, 2, rows, q, s, stream=0)
     with pytest.raises(TypeError):
         distdl.affine_fp8_fwd(nb, 64, 64, 2, "2", q, s, w8, ws, None, rows, stream=0)
+
+
+def test_packed_addresses_and_sizes_are_whole_ones():
+    """Bytes that end inside an address or a size are refused, in the calls that took lists alone before too."""
+    part = distdl.Partition((8, 8), (2, 2), (1, 1), (1, 1))
+    packed = np.array([256] * 4, np.int64).tobytes()
+    for cut in (1, 7, 8 * 4 - 1):
+        with pytest.raises(ValueError, match="addresses"):
+            distdl.halo_fwd(part, packed + b"\0" * cut, stream=0)
+        with pytest.raises(ValueError, match="addresses"):
+            distdl._calls.quantize_rows(4, 128, 1, packed[:8] + b"\0" * cut, 0, packed, packed, 0, 1, 1, 1)
+    with pytest.raises(distdl.DistdlError) as e:
+        distdl.halo_fwd(part, packed[:24], stream=0)
+    assert e.value.status == 1
+    a = torch.zeros(4)
+    for sizes in (b"", b"\4" + b"\0" * 7):
+        got = distdl._calls.check([a][:len(sizes) // 8], len(sizes) // 8, sizes, torch.float32, "a")
+        assert got == (b"",) if not sizes else got[0] == 1 and "host memory" in got[1]
+    with pytest.raises(ValueError, match="sizes"):
+        distdl._calls.check([a], 1, b"\4" + b"\0" * 8, torch.float32, "a")
