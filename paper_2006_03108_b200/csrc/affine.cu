@@ -102,6 +102,7 @@ struct AffinePairCfg {
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 /*alignment*/ + 256 /*barriers*/;
 };
+static_assert(tensor_blocks_fit(AffinePairCfg::SMEM_BYTES, kTileN), "affine_kernel_pair");
 
 __global__ void __launch_bounds__(kAffineThreads, 1)
 affine_kernel_pair(const __grid_constant__ AffineParams P) {
@@ -295,6 +296,18 @@ constexpr int kSplitWBytes = kTileM * kBlockK * 2;           // 16 KB: 128 featu
 constexpr int kSplitMaxStages = 12;
 constexpr int kSplitTail = 1024 + 256;                       // alignment, barriers
 constexpr int kSplitMaxSmem = 220 * 1024;                    // one block per SM; half of it: two
+constexpr int split_stage_bytes(int n) { return kSplitWBytes + n * kBlockK * 2; }
+constexpr int split_stages(int n, int budget) {
+    const int stages = (budget - kSplitTail) / split_stage_bytes(n);
+    return stages < kSplitMaxStages ? stages : kSplitMaxStages;
+}
+constexpr int split_smem(int n, int budget) { return split_stages(n, budget) * split_stage_bytes(n) + kSplitTail; }
+constexpr bool split_blocks_fit() {
+    bool fit = true;
+    for (int n = 16; n <= kTileM; n += 16) fit = fit && tensor_blocks_fit(split_smem(n, kSplitMaxSmem), 128) && tensor_blocks_fit(split_smem(n, kSplitMaxSmem / 2), 128);
+    return fit;
+}
+static_assert(split_blocks_fit(), "tensor_blocks_fit: affine_kernel_split");
 
 struct AffineSplitParams {
     AffineParams p;
@@ -483,6 +496,7 @@ constexpr int kQuadPitch = kQuadN / 2 + 4;                  // floats per row of
 constexpr int kQuadBufBytes = kTileM * kQuadPitch * 4;      // 67,584
 static_assert(3 * kQuadBufBytes <= kQuadStages * kQuadStageBytes, "epilogue buffers must fit in the ring");
 static_assert(kQuadBufBytes % 16 == 0, "bulk copies move multiples of 16 bytes");
+static_assert(tensor_blocks_fit(kQuadSmemBytes, kQuadN), "affine_kernel_quad");
 
 // shared memory of this block -> shared memory of another block of the cluster; the bytes are
 // counted on a barrier of the destination block
@@ -704,6 +718,7 @@ struct DwShape {                                             // tile 128 x TN
     static constexpr int kSmemBytes = kStages * kStageBytes + kDwOutBytes + 1024 + 128;
     static constexpr int kTmemCols = 2 * TN;                 // two accumulators
 };
+static_assert(tensor_blocks_fit(DwShape<128>::kSmemBytes, DwShape<128>::kTmemCols) && tensor_blocks_fit(DwShape<256>::kSmemBytes, DwShape<256>::kTmemCols), "affine_dw_kernel");
 
 struct AffineDwParams {
     CUtensorMap dy_map[8];                  // dy_i  [nb, bfo] bf16, box {64 out, 64 batch}
@@ -1089,10 +1104,10 @@ static distdl_status_t affine_impl(int64_t nb, int64_t nfi, int64_t nfo, int32_t
         Q.n = n_split;
         Q.split = 1;
         while (Q.split < 8 && ntiles * Q.split * 2 <= 2 * sms && all_kblocks >= 4 * 2 * Q.split) Q.split *= 2;
-        Q.stage_bytes = kSplitWBytes + Q.n * kBlockK * 2;
+        Q.stage_bytes = split_stage_bytes(Q.n);
         const int budget = ntiles * Q.split <= sms ? kSplitMaxSmem : kSplitMaxSmem / 2;
-        Q.stages = std::min(kSplitMaxStages, (budget - kSplitTail) / Q.stage_bytes);
-        const int smem = Q.stages * Q.stage_bytes + kSplitTail;       // at least three stages: room for the partial sums
+        Q.stages = split_stages(Q.n, budget);
+        const int smem = split_smem(Q.n, budget);                     // at least three stages: room for the partial sums
         launch_clusters_in_stream(affine_kernel_split, (unsigned)Q.split, dim3((unsigned)(ntiles * Q.split)), kAffineThreads, smem, (cudaStream_t)stream, Q);
     }
     DISTDL_CUDA_CHECK(cudaGetLastError());

@@ -138,6 +138,7 @@ struct F8Cfg {
     static constexpr int kSmemBytes = kStages * kStageBytes + kScaleBytes + kF8Tail;
     static_assert(kF8Rows * kPitch * 4 <= kStages * kStageBytes, "the sums take the ring's place");
     static_assert(TN % kScaleBlock == 0, "");
+    static_assert(tensor_blocks_fit(kSmemBytes, 512), "affine_fp8_pair_kernel");
     static constexpr int kBars = 2 * kStages + kBuffers + 2 * kF8ScaleSlots;
     static_assert(kBars * 8 + 8 <= 512, "barriers");
     // a stage's next product waits for the sums to have taken its last one: its barrier is never two turns ahead of them
@@ -553,11 +554,19 @@ struct F8FewCfg {
     static constexpr int kScaleBytes = 4 * kParts * 2 * kCols * 4;          // two sets of a k-block's scales for each summing warp
     static constexpr int kTail = kF8Tail + kScaleBytes;
     static constexpr int kMinStages = (512 * N + kStageBytes - 1) / kStageBytes;      // the sums take the ring's place
+    static constexpr int stages(int budget) { return (budget - kTail) / kStageBytes < kF8FewMaxStages ? (budget - kTail) / kStageBytes : kF8FewMaxStages; }
+    static constexpr int smem(int budget) { return stages(budget) * kStageBytes + kTail; }
     static_assert((2 * kF8FewMaxStages + kBuffers) * 8 + 8 <= 512, "barriers");
     static_assert((kF8FewMaxSmem / kBlocksPerSm - kTail) / kStageBytes >= kMinStages, "room for the sums");
     // a stage's next product waits for the sums to have taken its last one: its barrier is never two turns ahead of them
     static_assert((kF8FewMaxSmem / kBlocksPerSm - kTail) / kStageBytes >= kBuffers, "as many stages as products");
 };
+template <int N>
+constexpr bool few_blocks_fit() {
+    using C = F8FewCfg<N>;
+    return tensor_blocks_fit(C::smem(kF8FewMaxSmem), C::kTmemCols) && tensor_blocks_fit(C::smem(kF8FewMaxSmem / C::kBlocksPerSm), C::kTmemCols);
+}
+static_assert(few_blocks_fit<16>() && few_blocks_fit<32>() && few_blocks_fit<64>() && few_blocks_fit<128>(), "tensor_blocks_fit: affine_fp8_few_kernel");
 template <int C>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t *v) {
     if constexpr (C == 16) tmem_ld16(taddr, v);
@@ -817,8 +826,8 @@ static void launch_few(const AffineF8Params &P, int64_t tiles, int sms, cudaStre
     const int64_t all = (int64_t)P.nred * P.kpw;
     while (Q.split < 8 && tiles * Q.split * 2 <= C::kBlocksPerSm * sms && all >= 4 * 2 * Q.split) Q.split *= 2;
     const int budget = C::kBlocksPerSm == 1 || tiles * Q.split <= sms ? kF8FewMaxSmem : kF8FewMaxSmem / 2;
-    Q.stages = std::min(kF8FewMaxStages, (budget - C::kTail) / C::kStageBytes);
-    const int smem = Q.stages * C::kStageBytes + C::kTail;
+    Q.stages = C::stages(budget);
+    const int smem = C::smem(budget);
     launch_clusters_in_stream(affine_fp8_few_kernel<N>, (unsigned)Q.split, dim3((unsigned)(tiles * Q.split)), dim3(C::kThreads), (size_t)smem, stream, Q);
 }
 

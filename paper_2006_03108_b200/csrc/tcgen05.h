@@ -11,6 +11,19 @@
 
 namespace distdl {
 
+// tcgen05.alloc waits, without a limit of its own, until the columns that it asks for are there.  Kernels are launched while their predecessors run (see
+// stream_enter), and some ask for their columns ahead of their own wait, some behind it, when successors have been let in already: a block that waited for the
+// columns of another, which waits for the first one's kernel to end, would wait for good.  So no block of this library ever waits for columns: whatever
+// blocks of its tensor-memory kernels meet on a multiprocessor, there are 512 columns for all of them.  Shared memory sees to that.  Each takes enough of it
+// that there are at most two; a block with more than 256 columns takes so much that there is no second one.  Every such kernel states its
+// sizes to this function, beside its configuration.
+constexpr int kSmSharedBytes = 228 * 1024, kBlockSharedBytes = 1024;       // of a multiprocessor; what a block takes beside its own
+constexpr int kTensorSharedBytes = 80 * 1024;                              // a block with tensor memory takes at least that
+static_assert(3 * (kTensorSharedBytes + kBlockSharedBytes) > kSmSharedBytes, "at most two");
+constexpr bool tensor_blocks_fit(int smem, int columns) {
+    return smem >= kTensorSharedBytes && (columns <= 256 || (columns <= 512 && smem + kTensorSharedBytes + 2 * kBlockSharedBytes > kSmSharedBytes));
+}
+
 #ifdef __CUDACC__
 // Bounded wait: false if the limit ran out or another role already gave up.  The limit is counted
 // in SM clock cycles (reading %globaltimer costs several hundred nanoseconds, which would serialise
