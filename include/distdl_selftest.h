@@ -48,6 +48,13 @@ distdl_status_t distdl_selftest_conv_row_reads(const distdl_partition_t *p, int3
 distdl_status_t distdl_selftest_pool_adj_terms(const distdl_partition_t *p, int32_t k, int32_t stride, int32_t pad_lo, int32_t pad_hi,
                                                int32_t mode, int32_t worker, int32_t dim, int32_t *fused, int32_t *terms, int32_t num_terms);
 
+/* How the affine layer in 8 bits cuts a batch of more than 128 samples (adjoint != 0: the input gradient's): *columns of a tile (256 or 128), *runs that a
+ * tile's contraction is cut into (1, 2 or 4), *tiles, and *at_once, the clusters that the device holds at a time.  clusters: that number for each of the
+ * six kinds (256 columns in 1, 2, 4 runs, 128 columns in 1, 2, 4 runs), NULL: those of the current device.  Host only, but for that look at the
+ * device. */
+distdl_status_t distdl_selftest_affine_fp8_shape(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, int32_t adjoint, const int32_t *clusters,
+                                                 int32_t *columns, int32_t *runs, int64_t *tiles, int64_t *at_once);
+
 #ifdef __cplusplus
 }
 #endif

@@ -109,6 +109,7 @@ def lib():
     L.distdl_selftest_row_plan.argtypes = [vp, c_i32, pi32, c_i32, pi32, c_i32, pi32]
     L.distdl_selftest_conv_row_reads.argtypes = [vp, c_i32, c_i32, pi64, pi64]
     L.distdl_selftest_pool_adj_terms.argtypes = [vp] + [c_i32] * 7 + [pi32, pi32, c_i32]
+    L.distdl_selftest_affine_fp8_shape.argtypes = [c_i64, c_i64, c_i64, c_i32, c_i32, c_i32, pi32, pi32, pi32, pi64, pi64]
     _lib = L
     return L
 
@@ -759,3 +760,13 @@ def selftest_pool_adj_terms(part, kernel, stride, pad, mode, worker, dim):
     _check(lib().distdl_selftest_pool_adj_terms(part.handle, kernel, stride, pad[0], pad[1], mode, worker, dim, ctypes.byref(fused), terms,
                                                 kernel * cells))
     return fused.value, [list(terms[kernel * q:kernel * q + kernel]) for q in range(cells)] if fused.value else None
+
+
+def selftest_affine_fp8_shape(nb, nfi, nfo, pfo, pfi, adjoint=False, clusters=None):
+    """(columns of a tile, runs of its contraction, tiles, clusters at a time) of the affine layer in 8 bits on more than 128 samples; clusters: how many
+    of each of the six kinds a device holds, None: the current one's (include/distdl_selftest.h)."""
+    columns, runs, tiles, at_once = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int64(0), ctypes.c_int64(0)
+    held = None if clusters is None else (ctypes.c_int32 * 6)(*clusters)
+    _check(lib().distdl_selftest_affine_fp8_shape(nb, nfi, nfo, pfo, pfi, 1 if adjoint else 0, held, ctypes.byref(columns), ctypes.byref(runs),
+                                                  ctypes.byref(tiles), ctypes.byref(at_once)))
+    return columns.value, runs.value, tiles.value, at_once.value

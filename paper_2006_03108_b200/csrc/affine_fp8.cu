@@ -14,6 +14,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "distdl_selftest.h"
 #include "eight_bit.h"
 #include "tcgen05.h"
 #include "tma.h"
@@ -816,6 +817,59 @@ static const F8Shape kF8Shape[kF8Shapes] = {
     {affine_fp8_pair_kernel<128, true>, 128, 4, F8Cfg<128>::kThreads, F8Cfg<128>::kSmemBytes, 7.8, 0.0, 0.32},
 };
 
+// The shape for a layer of `all` k-blocks and nout output blocks of blk_out columns, its tiles and how many of its clusters run at a time; clusters: of each
+// shape.
+struct F8Choice {
+    const F8Shape *shape;
+    int64_t tiles, at_once;
+};
+static F8Choice f8_choose(int64_t nb, int nout, int64_t blk_out, int64_t all, const int *clusters) {
+    const int64_t row_tiles = (nb + 2 * kF8Rows - 1) / (2 * kF8Rows);
+    F8Choice c = {};
+    double best = 0;
+    for (int i = 0; i < kF8Shapes; ++i) {
+        const F8Shape &s = kF8Shape[i];
+        if ((s.splits > 1 && all < 4 * s.splits) || clusters[i] < 1) continue;
+        const int64_t tiles = row_tiles * nout * ((blk_out + s.tn - 1) / s.tn), turns = (tiles + clusters[i] - 1) / clusters[i];
+        const double again = s.splits > 1 ? s.first : s.next;
+        const double us = s.first + (double)turns * (double)((all + s.splits - 1) / s.splits) * s.kblock + (double)(turns - 1) * again;
+        if (!c.shape || us < best) {
+            best = us;
+            c = {&s, tiles, clusters[i]};
+        }
+    }
+    return c;
+}
+
+// One-time set-up of a device: kernel attributes, and how many clusters of each shape run at a time.
+static distdl_status_t f8_setup(int device, int sms, const int **clusters) {
+    static bool configured_on[kMaxDevicesPerProcess] = {false};
+    static int clusters_on[kMaxDevicesPerProcess][kF8Shapes];
+    std::lock_guard<std::mutex> setup_lock(setup_mutex());
+    if (!configured_on[device]) {
+        for (int i = 0; i < kF8Shapes; ++i) {
+            const F8Shape &s = kF8Shape[i];
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(2 * s.splits * sms));
+            cfg.blockDim = dim3((unsigned)s.threads);
+            cfg.dynamicSmemBytes = (size_t)s.smem;
+            cudaLaunchAttribute attr = {};
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 2u * s.splits;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            DISTDL_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&clusters_on[device][i], s.kernel, &cfg));
+        }
+        for (const auto kernel : {affine_fp8_few_kernel<16>, affine_fp8_few_kernel<32>, affine_fp8_few_kernel<64>, affine_fp8_few_kernel<128>})
+            DISTDL_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
+        configured_on[device] = true;
+    }
+    *clusters = clusters_on[device];
+    return DISTDL_OK;
+}
+
 template <int N>
 static void launch_few(const AffineF8Params &P, int64_t tiles, int sms, cudaStream_t stream) {
     // blocks of a tile: doubled while the device holds them all at a time and every block keeps four k-blocks
@@ -879,54 +933,16 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
         P.bias[i] = bias ? (const float *)bias[i] : nullptr;
     }
 
-    // one-time set-up per device: kernel attributes, and how many clusters of each kind run at a time
-    static bool configured_on[kMaxDevicesPerProcess] = {false};
-    static int clusters_on[kMaxDevicesPerProcess][kF8Shapes];
-    {
-        std::lock_guard<std::mutex> setup_lock(setup_mutex());
-        if (!configured_on[device]) {
-            for (int i = 0; i < kF8Shapes; ++i) {
-                const F8Shape &s = kF8Shape[i];
-                DISTDL_CUDA_CHECK(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
-                cudaLaunchConfig_t cfg = {};
-                cfg.gridDim = dim3((unsigned)(2 * s.splits * sms));
-                cfg.blockDim = dim3((unsigned)s.threads);
-                cfg.dynamicSmemBytes = (size_t)s.smem;
-                cudaLaunchAttribute attr = {};
-                attr.id = cudaLaunchAttributeClusterDimension;
-                attr.val.clusterDim.x = 2u * s.splits;
-                attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-                cfg.attrs = &attr;
-                cfg.numAttrs = 1;
-                DISTDL_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&clusters_on[device][i], s.kernel, &cfg));
-            }
-            for (const auto kernel : {affine_fp8_few_kernel<16>, affine_fp8_few_kernel<32>, affine_fp8_few_kernel<64>, affine_fp8_few_kernel<128>})
-                DISTDL_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8FewMaxSmem));
-            configured_on[device] = true;
-        }
-    }
+    const int *clusters;
+    if ((st = f8_setup(device, sms, &clusters))) return st;
     const bool few = nb <= kF8Rows;
     const int n = nb <= 16 ? 16 : nb <= 32 ? 32 : nb <= 64 ? 64 : 128;
-    const int64_t row_tiles = (nb + 2 * kF8Rows - 1) / (2 * kF8Rows), all = (int64_t)P.nred * P.kpw;
-    const F8Shape *shape = nullptr;
-    int64_t tiles = 0, at_once = 1;
+    F8Choice choice = {};
     if (!few) {
-        double best = 0;
-        for (int i = 0; i < kF8Shapes; ++i) {
-            const F8Shape &s = kF8Shape[i];
-            if ((s.splits > 1 && all < 4 * s.splits) || clusters_on[device][i] < 1) continue;
-            const int64_t n_tiles = row_tiles * nout * ((P.blk_out + s.tn - 1) / s.tn), turns = (n_tiles + clusters_on[device][i] - 1) / clusters_on[device][i];
-            const double again = s.splits > 1 ? s.first : s.next;
-            const double us = s.first + (double)turns * (double)((all + s.splits - 1) / s.splits) * s.kblock + (double)(turns - 1) * again;
-            if (!shape || us < best) {
-                best = us;
-                shape = &s;
-                tiles = n_tiles;
-                at_once = clusters_on[device][i];
-            }
-        }
-        if (!shape) return fail(DISTDL_ERR_CUDA, "%s: no cluster of two blocks fits the device", what);
+        choice = f8_choose(nb, nout, P.blk_out, (int64_t)P.nred * P.kpw, clusters);
+        if (!choice.shape) return fail(DISTDL_ERR_CUDA, "%s: no cluster of two blocks fits the device", what);
     }
+    const F8Shape *const shape = choice.shape;
     for (int i = 0; i < nact; ++i)
         if (!make_map_u8(&P.a_map[i], act[i], nb, P.blk_red, kF8K, few ? n : kF8Rows))
             return fail(DISTDL_ERR_CUDA, "%s: tensor map of activation block %d failed", what, i);
@@ -938,18 +954,18 @@ static distdl_status_t affine_fp8_impl(int64_t nb, int64_t nfi, int64_t nfo, int
     }
     const cudaStream_t in = (cudaStream_t)stream;
     if (few) {
-        tiles = nout * scale_blocks(P.blk_out);
+        const int64_t tiles = nout * scale_blocks(P.blk_out);
         if (n == 16) launch_few<16>(P, tiles, sms, in);
         else if (n == 32) launch_few<32>(P, tiles, sms, in);
         else if (n == 64) launch_few<64>(P, tiles, sms, in);
         else launch_few<128>(P, tiles, sms, in);
     } else {
-        if (tiles * 2 * shape->splits > INT32_MAX / 2) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
-        P.tiles = (int32_t)tiles;
+        if (choice.tiles * 2 * shape->splits > INT32_MAX / 2) return fail(DISTDL_ERR_UNSUPPORTED, "%s: too many tiles", what);
+        P.tiles = (int32_t)choice.tiles;
         P.splits = shape->splits;
-        const unsigned clusters = (unsigned)(shape->splits > 1 ? tiles : std::min(tiles, at_once));
+        const unsigned count = (unsigned)(shape->splits > 1 ? choice.tiles : std::min(choice.tiles, choice.at_once));
         const unsigned blocks = 2u * shape->splits;            // of a cluster
-        launch_clusters_in_stream(shape->kernel, blocks, dim3(blocks * clusters), dim3((unsigned)shape->threads), (size_t)shape->smem, in, P);
+        launch_clusters_in_stream(shape->kernel, blocks, dim3(blocks * count), dim3((unsigned)shape->threads), (size_t)shape->smem, in, P);
     }
     DISTDL_CUDA_CHECK(cudaGetLastError());
     return DISTDL_OK;
@@ -967,4 +983,30 @@ extern "C" distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_
                                                  const void *const *dys, const void *const *w, const void *const *ws, distdl_dtype_t t, void *const *dx,
                                                  void *stream) {
     return distdl::affine_fp8_impl(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, nullptr, t, dx, stream, true, "affine_fp8_adj");
+}
+
+extern "C" distdl_status_t distdl_selftest_affine_fp8_shape(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, int32_t adjoint,
+                                                            const int32_t *clusters, int32_t *columns, int32_t *runs, int64_t *tiles, int64_t *at_once) {
+    using namespace distdl;
+    const char *what = "selftest_affine_fp8_shape";
+    clear_error();
+    if (!columns || !runs || !tiles || !at_once) return fail(DISTDL_ERR_INVALID_ARG, "%s: NULL argument", what);
+    if (nb <= kF8Rows || nfi < 1 || nfo < 1 || pfo < 1 || pfi < 1 || nfi % pfi || nfo % pfo) return fail(DISTDL_ERR_INVALID_ARG, "%s: sizes", what);
+    if (!clusters) {
+        int device, sms;
+        const int *found;
+        DISTDL_CUDA_CHECK(cudaGetDevice(&device));
+        if (device < 0 || device >= kMaxDevicesPerProcess) return fail(DISTDL_ERR_UNSUPPORTED, "%s: device index %d", what, device);
+        if (const distdl_status_t st = multiprocessors(device, &sms)) return st;
+        if (const distdl_status_t st = f8_setup(device, sms, &found)) return st;
+        clusters = found;
+    }
+    const int64_t bfi = nfi / pfi, bfo = nfo / pfo;
+    const F8Choice c = f8_choose(nb, adjoint ? pfi : pfo, adjoint ? bfi : bfo, adjoint ? pfo * scale_blocks(bfo) : pfi * scale_blocks(bfi), clusters);
+    if (!c.shape) return fail(DISTDL_ERR_CUDA, "%s: no cluster of two blocks fits the device", what);
+    *columns = c.shape->tn;
+    *runs = c.shape->splits;
+    *tiles = c.tiles;
+    *at_once = c.at_once;
+    return DISTDL_OK;
 }

@@ -6,7 +6,7 @@ import pytest
 import paper_2006_03108_b200 as distdl
 from oracle import eight_bit as o
 from paper_2006_03108_b200 import inputs
-from test_eight_bit_gpu import DEV, E4, U, Out, dev, eps_of, f64, rounded, sum_error
+from test_eight_bit_gpu import DEV, E4, FP8, U, Out, dev, eps_of, f64, rounded, sum_error
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,71 @@ def test_adamw_writes_nothing_once_a_tensor_has_moved(eight):
     distdl.AdamW(p, *state, *scales).step(g, 1e-3, 2)
     torch.cuda.synchronize()
     assert not torch.equal(p[1], before[1]) and torch.equal(old, before[1])
+
+
+# Batches that the other tests' sizes leave to none: nb, contraction, columns of a result, workers of either, (columns of a tile, runs of its contraction).
+# 256 columns in four runs -- whole, ragged, more than one worker -- and in two, in one turn and in three
+RUNS = [(200, 16384, 2816, 1, 1, (256, 4)), (250, 16384, 2800, 1, 1, (256, 4)), (129, 8192, 1408, 2, 2, (256, 4)), (256, 16400, 2576, 1, 1, (256, 4)),
+        (1200, 4992, 1040, 2, 1, (256, 2)), (900, 13472, 4800, 1, 1, (256, 2))]
+
+
+def runs_case(case, adj):
+    """nb, features of a worker's input and output block, grid (outputs, inputs)."""
+    nb, red, out, workers_red, workers_out, _ = case
+    return (nb, out, red, workers_red, workers_out) if adj else (nb, red, out, workers_out, workers_red)
+
+
+@pytest.mark.parametrize("exact", [True, False], ids=["whole", "normal"])
+@pytest.mark.parametrize("adj", [False, True], ids=["fwd", "adj"])
+@pytest.mark.parametrize("case", RUNS, ids=str)
+def test_affine_fp8_in_runs_of_the_contraction(case, adj, exact):
+    """Against products in 64 bits on the device: whole numbers, whose sums are exact in fp32 (at most 2^15 of 64), to the bit; normal ones as in
+    test_eight_bit_gpu.py."""
+    nb, bfi, bfo, pfo, pfi = runs_case(case, adj)
+    shape = distdl.selftest_affine_fp8_shape(nb, bfi * pfi, bfo * pfo, pfo, pfi, adj)
+    assert shape[:2] == case[5], shape
+    g = torch.Generator(device=DEV)
+    g.manual_seed(sum(case[:5]) + adj)
+    ki, ko = -(-bfi // 128), -(-bfo // 128)
+    (red, kr, nred), (blk, nout) = ((bfo, ko, pfo), (bfi, pfi)) if adj else ((bfi, ki, pfi), (bfo, pfo))
+    whole = lambda lo, hi, *s: torch.randint(lo, hi, s, device=DEV, generator=g)  # noqa: E731
+    normal = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    e = lambda *s, dtype=torch.float32: torch.empty(*s, device=DEV, dtype=dtype)  # noqa: E731
+    if exact:
+        a, asc = [whole(-2, 3, nb, red).float().to(E4) for _ in range(nred)], [torch.exp2(whole(0, 3, kr, nb).float()) for _ in range(nred)]
+        w, wsc = [whole(-2, 3, bfo, bfi).float().to(E4) for _ in range(pfo * pfi)], [torch.exp2(whole(0, 3, ko, ki).float()) for _ in range(pfo * pfi)]
+        bias = [whole(-9, 10, blk).float() for _ in range(nout)]
+    else:
+        a, asc, w, wsc = [e(nb, red, dtype=E4) for _ in range(nred)], [e(kr, nb) for _ in range(nred)], [e(bfo, bfi, dtype=E4) for _ in range(pfo * pfi)], [e(ko, ki) for _ in range(pfo * pfi)]
+        distdl.quantize_rows(nb, red * nred, nred, [normal(nb, red) for _ in range(nred)], a, asc)
+        distdl.quantize_weights(bfi * pfi, bfo * pfo, pfo, pfi, [normal(bfo, bfi) * 0.05 for _ in range(pfo * pfi)], w, wsc)
+        bias = [normal(blk) for _ in range(nout)]
+    av = [q.double() * s.double().t().repeat_interleave(128, 1)[:, :red] for q, s in zip(a, asc)]
+    wv = [q.double() * s.double().repeat_interleave(128, 0)[:bfo].repeat_interleave(128, 1)[:, :bfi] for q, s in zip(w, wsc)]
+    for t in (torch.float32, torch.bfloat16):
+        out = Out()
+        y = [out(nb, blk, dtype=t) for _ in range(nout)]
+        if adj:
+            distdl.affine_fp8_adj(nb, bfi * pfi, bfo * pfo, pfo, pfi, a, asc, w, wsc, y)
+        else:
+            distdl.affine_fp8_fwd(nb, bfi * pfi, bfo * pfo, pfo, pfi, a, asc, w, wsc, bias, y)
+        distdl.device_status()
+        for j in range(nout):
+            pairs = [(av[i], wv[i * pfi + j] if adj else wv[j * pfi + i].t()) for i in range(nred)]
+            want, size = sum(x @ v for x, v in pairs), sum(x.abs() @ v.abs() for x, v in pairs)
+            if not adj:
+                want, size = want + bias[j].double(), size + bias[j].double().abs()
+            if exact:
+                assert torch.equal(y[j].double(), want.float().to(t).double())
+            else:
+                err = (2 * 128 + 2 + kr * nred + 8) * U * size
+                assert ((y[j].double() - want).abs() <= err + eps_of(t) * (want.abs() + err)).all()
+        out.check()
+
+
+def test_affine_fp8_cases_reach_every_shape_of_this_device():
+    """As in the CPU test of the same rule, with the clusters that this device holds."""
+    for adj in (False, True):
+        cases = [c for c in FP8 if c[0] > 128] + [runs_case(c, adj) for c in RUNS]
+        seen = {distdl.selftest_affine_fp8_shape(c[0], c[1] * c[4], c[2] * c[3], c[3], c[4], adj)[:2] for c in cases}
+        assert seen == {(n, r) for n in (256, 128) for r in (1, 2, 4)}, seen

@@ -102,3 +102,29 @@ def test_packed_addresses_and_sizes_are_whole_ones():
         assert got == (b"",) if not sizes else got[0] == 1 and "host memory" in got[1]
     with pytest.raises(ValueError, match="sizes"):
         distdl._calls.check([a], 1, b"\4" + b"\0" * 8, torch.float32, "a")
+
+
+@pytest.mark.parametrize("clusters", [(74, 37, 18, 74, 37, 18), (74, 35, 16, 74, 35, 16), (74, 33, 15, 74, 33, 15), (70, 31, 12, 70, 31, 12)], ids=str)
+def test_affine_fp8_cases_reach_every_shape(clusters):
+    """The sizes that the GPU tests run take the 8-bit layer through all six of its shapes, forward and back: a measured time that is set anew cannot leave
+    one untested without a word.  clusters: how many of each shape a device of 148 multiprocessors may hold."""
+    from test_eight_bit_gpu import FP8
+    from test_eight_bit_limits_gpu import RUNS, runs_case
+    for adj in (False, True):
+        seen = {}
+        for c in [c for c in FP8 if c[0] > 128] + [runs_case(c, adj) for c in RUNS]:
+            got = distdl.selftest_affine_fp8_shape(c[0], c[1] * c[4], c[2] * c[3], c[3], c[4], adj, clusters)
+            seen.setdefault(got[:2], []).append(got[2] > got[3])
+        assert set(seen) == {(n, r) for n in (256, 128) for r in (1, 2, 4)}, seen
+        assert all(any(seen[k]) for k in ((256, 1), (256, 2))) and not all(seen[256, 2])           # in one turn and in several
+        for c in RUNS:
+            n = runs_case(c, adj)
+            assert distdl.selftest_affine_fp8_shape(n[0], n[1] * n[4], n[2] * n[3], n[3], n[4], adj, clusters)[:2] == c[5], c
+    # what a tile costs decides; a shape that the device cannot hold is never taken
+    assert distdl.selftest_affine_fp8_shape(200, 16384, 2816, 1, 1, False, (74, 37, 0, 74, 37, 0))[1] != 4
+    with pytest.raises(distdl.DistdlError):
+        distdl.selftest_affine_fp8_shape(200, 16384, 2816, 1, 1, False, (0,) * 6)
+    for bad in ((128, 128, 128, 1, 1), (200, 128, 130, 4, 1), (200, 0, 128, 1, 1)):
+        with pytest.raises(distdl.DistdlError) as e:
+            distdl.selftest_affine_fp8_shape(*bad, False, clusters)
+        assert e.value.status == 1
