@@ -442,7 +442,6 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
                     for (int i = 0; i < 32; ++i)                            // two sums at an instruction
                         acc[c / 2 + i] = __ffma2_rn(make_float2(now, now), make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), acc[c / 2 + i]);
                 }
-                if (!ok) break;
                 if (++s == C::kStages) {
                     s = 0;
                     phase ^= 1;
@@ -548,7 +547,6 @@ struct F8FewCfg {
     static constexpr int kCols = N / kParts;
     static constexpr int kThreads = 128 + 128 * kParts;     // warp 0: TMA, 1: MMA and tensor memory, 3: MMA, 4..: sums
     static constexpr int kBlocksPerSm = N >= 64 ? 1 : 2;
-    static constexpr int kLoad = kCols;                     // columns that a tensor-memory load takes
     static constexpr int kStageBytes = kF8WBytes + N * kF8K;
     static constexpr int kBuffers = N >= 128 ? 2 : 4;       // products in tensor memory
     static constexpr int kTmemCols = kBuffers * N;
@@ -720,22 +718,17 @@ affine_fp8_few_kernel(const __grid_constant__ AffineF8FewParams Q) {
                 ok = __all_sync(0xffffffffu, f8_wait(bar_done + 8 * s, phase, abort_flag));
                 if (!ok) break;
                 tcgen05_fence_after();
+                uint32_t v[C::kCols];
+                tmem_ld<C::kCols>(taddr + buf * N, v);
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_free + 8 * buf);
 #pragma unroll
-                for (int c = 0; c < C::kCols; c += C::kLoad) {
-                    uint32_t v[C::kLoad];
-                    tmem_ld<C::kLoad>(taddr + buf * N + c, v);
-                    if (c + C::kLoad == C::kCols) {
-                        tcgen05_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bar_free + 8 * buf);
-                    }
-#pragma unroll
-                    for (int i = 0; i < C::kLoad; i += 4) {
-                        const float4 f = *reinterpret_cast<const float4 *>(set + c + i);
-                        float2 &lo = acc[(c + i) / 2], &hi = acc[(c + i) / 2 + 1];
-                        lo = __ffma2_rn(make_float2(f.x, f.y), make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), lo);
-                        hi = __ffma2_rn(make_float2(f.z, f.w), make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), hi);
-                    }
+                for (int i = 0; i < C::kCols; i += 4) {
+                    const float4 f = *reinterpret_cast<const float4 *>(set + i);
+                    float2 &lo = acc[i / 2], &hi = acc[i / 2 + 1];
+                    lo = __ffma2_rn(make_float2(f.x, f.y), make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), lo);
+                    hi = __ffma2_rn(make_float2(f.z, f.w), make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), hi);
                 }
                 if (++s == (uint32_t)stages) {
                     s = 0;
