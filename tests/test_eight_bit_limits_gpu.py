@@ -158,3 +158,32 @@ def test_affine_fp8_cases_reach_every_shape_of_this_device():
         cases = [c for c in FP8 if c[0] > 128] + [runs_case(c, adj) for c in RUNS]
         seen = {distdl.selftest_affine_fp8_shape(c[0], c[1] * c[4], c[2] * c[3], c[3], c[4], adj)[:2] for c in cases}
         assert seen == {(n, r) for n in (256, 128) for r in (1, 2, 4)}, seen
+
+
+def test_adamw_codes_in_8_bits_decay_under_a_scale_that_stays():
+    """One element of each block has a gradient that keeps both its moments, and so the block's scale, where they are; the others have none, and their
+    codes have to fall by beta (its root) a step, 0.5 % and 0.05 %, where the codes are 6 to 12 % apart.  Rounded to nearest none would ever move.
+
+    A value x on a code, w = x / 8 at most above the next one, moves down by it with probability (1 - beta) x / w: it keeps the mean, with a variance of
+    (1 - beta) x w <= (1 - beta) x^2 / 8.  After n steps that is (1 + (1 - beta) / 8 / beta^2)^n - 1 of the squared mean or less; six deviations of the mean of
+    all elements, and the kept moments' own roundings (2 U a step)."""
+    n, steps, b1, b2 = 4096, 400, 0.995, 0.999
+    p, g = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    m, v = [torch.full((n,), 288.0, device=DEV).to(E4) for _ in range(2)]
+    ms, vs = [torch.ones(n // 128, device=DEV) for _ in range(2)]
+    m[::128], v[::128], g[::128] = 448.0, 448.0, 448.0
+    opt = distdl.AdamW([p], [m], [v], [ms], [vs])
+    for t in range(steps):
+        opt.step([g], 1e-3, 10 + t, betas=(b1, b2), seed=17)
+    rest = np.arange(n) % 128 != 0
+    for code, scale, beta in ((m, ms, b1), (v, vs, b2 ** 0.5)):
+        c, s = f64(code), f64(scale)
+        assert (c[~rest] == 448).all() and (np.abs(s - 1) <= 4 * steps * U).all()
+        spread = np.sqrt(((1 + (1 - beta) / 8 / beta ** 2) ** steps - 1) / rest.sum())
+        bound = 6 * spread + 4 * steps * U
+        mean = (c * np.repeat(s, 128))[rest].mean() / 288
+        assert abs(mean / beta ** steps - 1) <= bound, (mean, beta ** steps, bound)
+        nearest = np.full(4, 288.0)
+        for _ in range(steps):
+            nearest = o.e4m3_round(nearest * beta)
+        assert (nearest == 288).all() and abs(nearest.mean() / 288 / beta ** steps - 1) > bound
