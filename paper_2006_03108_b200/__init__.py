@@ -560,9 +560,7 @@ def _need(*lists):
     return found
 
 
-def _whole(*numbers):
-    """Whole numbers of any type with __index__, as Python's: products of NumPy's 32-bit ones would wrap around."""
-    return map(operator.index, numbers)
+_whole = operator.index                                # a whole number of any type as Python's: products of NumPy's 32-bit ones would wrap around
 
 
 def _features(what, n, workers):
@@ -578,7 +576,7 @@ def _blocks128(n):
 def quantize_rows(nb, nf, pf, x, q, s, stream=None):
     """Values of x[j] [nb, nf/pf] in 8 bits, q[j] float8_e4m3fn, and a scale for every 128 features of a row, s[j] float32
     [ceil((nf/pf)/128), nb]."""
-    nb, nf, pf = _whole(nb, nf, pf)
+    nb, nf, pf = _whole(nb), _whole(nf), _whole(pf)
     code, dtype = _float_code("x", x)
     bf = _features("quantize_rows", nf, pf)
     n = nb * bf
@@ -589,7 +587,7 @@ def quantize_rows(nb, nf, pf, x, q, s, stream=None):
 def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
     """Blocks of weights w[i * pfi + j] [nfo/pfo, nfi/pfi] in 8 bits, q float8_e4m3fn, and a scale for every 128 x 128, s float32
     [ceil((nfo/pfo)/128), ceil((nfi/pfi)/128)]."""
-    nfi, nfo, pfo, pfi = _whole(nfi, nfo, pfo, pfi)
+    nfi, nfo, pfo, pfi = _whole(nfi), _whole(nfo), _whole(pfo), _whole(pfi)
     code, dtype = _float_code("w", w)
     bfi, bfo, n = _features("quantize_weights", nfi, pfi), _features("quantize_weights", nfo, pfo), pfo * pfi
     w, q, s = _need(w, n, bfo * bfi, dtype, "w", q, n, bfo * bfi, _types["e4m3"], "q", s, n, _blocks128(bfo) * _blocks128(bfi), _types["f32"], "s")
@@ -599,7 +597,7 @@ def quantize_weights(nfi, nfo, pfo, pfi, w, q, s, stream=None):
 def rmsnorm_fwd(nb, nf, pf, x, residual, gamma, eps, h=None, y=None, q=None, qs=None, rstd=None, stream=None):
     """h = x + residual (residual None: x), rstd = 1 / sqrt(mean h^2 + eps), h * rstd * gamma as y (type of x) and / or as q, qs in 8
     bits; each output may be None.  Lists of feature blocks [nb, nf/pf]; h may be the residual's own blocks."""
-    nb, nf, pf = _whole(nb, nf, pf)
+    nb, nf, pf = _whole(nb), _whole(nf), _whole(pf)
     code, dtype = _float_code("x", x)
     bf = _features("rmsnorm_fwd", nf, pf)
     n, f32 = nb * bf, _types["f32"]
@@ -619,7 +617,7 @@ def rmsnorm_adj_workspace(nb, nf, pf):
 def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, stream=None):
     """Gradient dh of x and of the residual (dres: the gradient that reaches their sum past the norm, or None), and dgamma (or None);
     h and rstd as rmsnorm_fwd left them; workspace: a uint8 tensor."""
-    nb, nf, pf = _whole(nb, nf, pf)
+    nb, nf, pf = _whole(nb), _whole(nf), _whole(pf)
     code, dtype = _float_code("h", h)
     gcode, gdtype = _float_code("dy", dy)
     bf = _features("rmsnorm_adj", nf, pf)
@@ -633,7 +631,7 @@ def rmsnorm_adj(nb, nf, pf, dy, dres, h, gamma, rstd, dh, dgamma, workspace, str
 
 def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
     """y_i = sum over j of x_j W_ij^T (+ bias_i) with x, xs as quantize_rows and w, ws as quantize_weights leave them; y float32 or bfloat16."""
-    nb, nfi, nfo, pfo, pfi = _whole(nb, nfi, nfo, pfo, pfi)
+    nb, nfi, nfo, pfo, pfi = _whole(nb), _whole(nfi), _whole(nfo), _whole(pfo), _whole(pfi)
     code, dtype = _float_code("y", y)
     bfi, bfo = _features("affine_fp8_fwd", nfi, pfi), _features("affine_fp8_fwd", nfo, pfo)
     ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
@@ -645,7 +643,7 @@ def affine_fp8_fwd(nb, nfi, nfo, pfo, pfi, x, xs, w, ws, bias, y, stream=None):
 
 def affine_fp8_adj(nb, nfi, nfo, pfo, pfi, dy, dys, w, ws, dx, stream=None):
     """dx_j = sum over i of dy_i W_ij with dy, dys as quantize_rows and w, ws as quantize_weights leave them; dx float32 or bfloat16."""
-    nb, nfi, nfo, pfo, pfi = _whole(nb, nfi, nfo, pfo, pfi)
+    nb, nfi, nfo, pfo, pfi = _whole(nb), _whole(nfi), _whole(nfo), _whole(pfo), _whole(pfi)
     code, dtype = _float_code("dx", dx)
     bfi, bfo = _features("affine_fp8_adj", nfi, pfi), _features("affine_fp8_adj", nfo, pfo)
     ki, ko, n, e4m3, f32 = _blocks128(bfi), _blocks128(bfo), pfo * pfi, _types["e4m3"], _types["f32"]
