@@ -475,7 +475,8 @@ distdl_status_t distdl_quantize_weights(int64_t nfi, int64_t nfo, int32_t pfo, i
  *     y = h * rstd * gamma, as y[j] rounded to t and / or as q[j], qs[j] in 8 bits (quantize_rows of the fp32 value).
  *   x[j], residual[j] [nb, nf/pf] of type t (F32 or BF16); gamma[j] F32 [nf/pf]; eps: HOST pointer to one value >= 2^-120.
  *   Outputs, each list NULL if not wanted: h[j] (may be the residual's or x's own buffers: the sum in place), y[j] of type t,
- *   q[j] with qs[j]; rstd F32 [nb] or NULL.  y[j] may be x's buffers; no other overlap.  Sums in fp32.
+ *   q[j] with qs[j]; rstd F32 [nb] or NULL.  y[j] may be x's buffers; no other overlap.  Sums in fp32: a sample whose squares add up to
+ *   2^128 or more (no value below 2^53 in magnitude makes that) has rstd = 0.
  * rmsnorm_adj, with h and rstd of the forward pass:
  *     dh = dres + rstd * (gamma dy - hhat * mean over f of (gamma dy hhat)),  hhat = h * rstd;
  *     dgamma[f] = sum over b of dy hhat.
@@ -511,7 +512,8 @@ distdl_status_t distdl_rmsnorm_adj(int64_t nb, int64_t nf, int32_t pf, const voi
  * product is taken in fp32) and added to an fp32 sum, in the workers' and blocks' order -- in up to eight runs of that order, whose
  * sums are added up in order, where one run would leave SMs idle.  Rounded once, to t, with the bias.
  * nfi % Pfi == 0, nfo % Pfo == 0 (else DISTDL_ERR_SHAPE); the per-worker block sizes must be multiples of 16, Pfo, Pfi <= 8 and
- * Pfo * Pfi <= 16 (else DISTDL_ERR_UNSUPPORTED); 1 <= nb <= 2^20.  dW and db: distdl_affine_adj_params on the bfloat16 values.
+ * Pfo * Pfi <= 16 (else DISTDL_ERR_UNSUPPORTED); 1 <= nb <= 2^20.  dW and db: distdl_affine_adj_params, which takes x and dy as BF16: the
+ * y of rmsnorm_fwd with t = BF16, or an F32 one that the caller has converted.
  * A launch whose device-side waits ran out reports through distdl_device_status().
  * ---------------------------------------------------------------------- */
 distdl_status_t distdl_affine_fp8_fwd(int64_t nb, int64_t nfi, int64_t nfo, int32_t pfo, int32_t pfi, const void *const *x,
@@ -538,10 +540,11 @@ distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_t nfo, int3
  *     The step itself uses the moments before they are rounded.
  * hyper: HOST array {lr, beta1, beta2, eps, decay, c}, eps >= 2^-120;  step: t >= 1, the same for all tensors.
  * live: NULL, or a DEVICE array F32 {lr, t, c} that is read when the step runs and stands in the place of those three, for
- *     steps that are captured in a graph and replayed (t is exact up to 2^24).
+ *     steps that are captured in a graph and replayed (1 <= t; exact up to 2^24).
  * count <= DISTDL_MAX_TENSORS.  One launch for every 320 tensors.  Buffers that are written may not overlap any other
  * buffer of the call (not detected: undefined results).  Every element's result depends on that element, and in 8 bits on
- * its block of 128, alone; fp32 throughout.
+ * its block of 128, alone.  fp32 throughout, root and quotient of the step approximate (to some 2^-22); so are squares: of a gradient |c g|
+ * below 2^-63 the second moment keeps fewer digits or none, above 2^64 or so it is infinite, and with it a block held in 8 bits.
  * ---------------------------------------------------------------------- */
 #define DISTDL_MAX_TENSORS 4096
 distdl_status_t distdl_adamw_step(int32_t count, const int64_t *elems, void *const *p, const void *const *g,

@@ -113,9 +113,11 @@ __device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
 // k-blocks of a tile, in S runs one after the other, and adds up the S sums through distributed shared memory in that order.
 //
 // What bounds it.  The tensor cores take 600 clocks for a k-block of a 256 x 256 tile, and 32 KB for it come into each SM.  Large products run at what
-// power and L2 allow: 2048 x 8192 x 8192 in 127 us (2160 TFLOP/s; 11 TB/s from L2) in a burst, 4096 x 8192 x 8192 in 235 us, 274 us (2010 TFLOP/s at 1.48
+// power and L2 allow: 2048 x 8192 x 8192 in 127 to 132 us from machine to machine (2080 to 2160 TFLOP/s; 1.07 GB from L2, 8.1 to 8.5 TB/s) in a burst,
+// 4096 x 8192 x 8192 in 235 to 245 us, 274 us (2010 TFLOP/s at 1.48
 // GHz and 1 kW) when it goes on for seconds -- the same loop with all k-blocks added up in tensor memory, without scales, takes 218 and 250.  Small ones
-// are bound by what surrounds the k-blocks, some 5 to 8 us: 256 x 8192 x 8192 25 us, 777 x 3120 x 1312 13.5 us.  On the way (2048 x 8192 x 8192, us): an
+// are bound by what surrounds the k-blocks, some 5 to 8 us: 256 x 8192 x 8192 26 us (adjoint 25), 777 x 3120 x 1312 14.6 us.  256 columns in runs spill 36
+// bytes a thread.  On the way (2048 x 8192 x 8192, us): an
 // arrival at the other block with release at the cluster's scope, a fence for every warp and k-block, 336; without 192; scalar sums instead of pairs put
 // together by moves 167; pairs that go on from tile to tile 152; one barrier for a product and its stage instead of two 143; eight summing warps with
 // 64-column loads instead of sixteen with 32-column ones 135; a second thread that issues products 127. Halves of tiles for the last turn cost the other
@@ -530,8 +532,8 @@ affine_fp8_pair_kernel(const __grid_constant__ AffineF8Params P) {
 // Few samples (a batch of at most 128): the weights are the M operand, 128 output features a block, the batch takes N = 16, 32, 64 or 128 columns.  A
 // cluster of S blocks shares the k-blocks of the features in S runs and adds up the S sums through distributed shared memory in that order.  What bounds it
 // is the stream of the weights: two blocks an SM (one from N = 64 on, whose sums need the registers of two) keep it going, and its first copies leave
-// before anything else is set up.  8192 x 8192 weights (B200, cold, in a graph): one sample 15.2 us -- of which the weights take 10.4 at the copy rate,
-// from 0.7 us after the start on -- 32 samples 16.5, 64 19.0, 128 22.0.
+// before anything else is set up.  8192 x 8192 weights (B200, cold, in a graph): one sample 16.0 us (adjoint 15.5) -- of which the weights take 10.4 at the copy
+// rate, from 0.7 us after the start on -- 32 samples 17.2, 64 19.9, 128 22.7.
 // ------------------------------------------------------------------------------------------
 constexpr int kF8WBytes = 128 * kF8K;
 constexpr int kF8FewMaxStages = 12;

@@ -21,7 +21,7 @@ struct QuantRowsParams {
 };
 
 // What bounds it: HBM, read once and written once.  B200: 8192 x 8192 bf16 36.5 us (5.6 TB/s), 4096 x 8192 fp32 28.5 (5.9); rows of 1001, which take
-// 2-byte loads and byte stores, 32.8 us for 8192 x 4004 (3.0 TB/s); 256 x 8192, in a graph, 2.7 us.
+// 2-byte loads and byte stores whose number is what counts, 32.8 us for 8192 x 4004 (3.0 TB/s); 256 x 8192, in a graph, 2.4 us with x in L2, 3.5 from HBM.
 // A thread block takes kSpan blocks side by side of rows r0, r0 + 1, ...: half a warp a block and row, kDepth rows of each in flight.  The scales of a block
 // lie row by row, so those of the thread block's rows fill whole lines in L2 before they leave.
 constexpr int kSpan = 4;

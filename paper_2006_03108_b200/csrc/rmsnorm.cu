@@ -129,8 +129,9 @@ __device__ __forceinline__ void norm_write(const NormParams &P, int64_t row, con
 // V: chunks of a thread, which stay in registers between the two passes over the sample; 0: any number, read again.
 //
 // What bounds it: HBM for many samples -- every input is read once and every output written once -- and the latency of one pass for few.  B200, bf16 with
-// residual, h, y, q: 8192 x 8192 on four workers 106 us (5.7 TB/s, 0.88 of the copy rate), 8192 x 4096 53 (5.7), 32768 x 512 29 (5.2), 4000 x 2 x 1415
-// (2-byte loads) 39 (2.6); one sample of 8192 in a graph 3.7 us.
+// residual, h, y, q: 8192 x 8192 on four workers 107 us (5.7 TB/s, 0.87 of the copy rate), 8192 x 4096 53 (5.7), 32768 x 512 29 (5.2), 4000 x 2 x 1415
+// 39 (2.6; an access of 2 bytes for every value, and their number is what counts); fp32 8192 x 8192 207 (5.5); one sample of 8192 with h, q in a graph 3.3 us.
+// Four chunks in bfloat16 spill 48 bytes of a thread's 64 registers.
 template <typename T, int VW, int V>
 __global__ void __launch_bounds__(kNormMaxThreads)
 rmsnorm_kernel(const __grid_constant__ NormParams P) {
@@ -248,8 +249,10 @@ constexpr int adj_resident(bool all_bf16, int v) { return v > 1 ? 512 : all_bf16
 // dy and h are read twice then).
 //
 // What bounds it: HBM, with one sample in work and the next on its way in every thread block; a thread block a sample and multiprocessor in flight reached
-// half of it. B200, with dres, the fold of dgamma included: 8192 x 8192 bf16 92 us (5.9 TB/s, 0.9 of the copy rate), 8192 x 4096 48 (5.6), 4096 x 4096 fp32
-// 46 (5.9), 1021 x 5000 fp32 in rows of 1250 (8-byte loads) 18 (4.5), 1000 x 32768 bf16 73 (3.6; 5.4 with what is read twice).
+// half of it. B200, with dres, the fold of dgamma included: 8192 x 8192 bf16 92 us (5.8 TB/s, 0.9 of the copy rate), 8192 x 4096 48 (5.6), 4096 x 4096 fp32
+// 46 (5.9), 1021 x 5000 fp32 in rows of 1250 (8-byte loads) 18.5 (4.4), 1000 x 32768 bf16 74 (3.5; 5.3 with what is read twice). Two chunks without look-ahead,
+// beyond 5120 features with a 32-bit type, lose nothing by it: 8192 x 8192 bf16 with fp32 gradients 158 (5.9), fp32 171 (6.3); 4096 x 5120 with one chunk
+// 51 (5.7).  Four in bfloat16, beyond 8192 features, do, and spill 116 to 280 bytes a thread: 4096 x 12288 119 (3.4), 4096 x 16384 135 (4.0).
 template <typename T, typename TG, int VW, int V, bool GIVEN>
 __global__ void __launch_bounds__(adj_resident(sizeof(T) + sizeof(TG) <= 4, V), 1)
 rmsnorm_adj_kernel(const __grid_constant__ NormAdjParams P) {
