@@ -543,8 +543,8 @@ distdl_status_t distdl_affine_fp8_adj(int64_t nb, int64_t nfi, int64_t nfo, int3
  *     steps that are captured in a graph and replayed (1 <= t; exact up to 2^24).
  * count <= DISTDL_MAX_TENSORS.  One launch for every 320 tensors.  Buffers that are written may not overlap any other
  * buffer of the call (not detected: undefined results).  Every element's result depends on that element, and in 8 bits on
- * its block of 128, alone.  fp32 throughout, root and quotient of the step approximate (to some 2^-22); so are squares: of a gradient |c g|
- * below 2^-63 the second moment keeps fewer digits or none, above 2^64 or so it is infinite, and with it a block held in 8 bits.
+ * its block of 128, alone.  fp32 throughout; root and quotient of the step are approximate (to some 2^-22).  Squares are fp32 too: of a gradient
+ * with |c g| below 2^-63 the second moment keeps fewer digits or none, above 2^64 or so it is infinite (in 8 bits: its whole block is lost).
  * ---------------------------------------------------------------------- */
 #define DISTDL_MAX_TENSORS 4096
 distdl_status_t distdl_adamw_step(int32_t count, const int64_t *elems, void *const *p, const void *const *g,

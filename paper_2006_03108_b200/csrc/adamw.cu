@@ -92,10 +92,10 @@ __device__ __forceinline__ void adam_pair(const AdamCommon &P, const AdamStep &s
 }
 
 // What bounds it: HBM with fp32 states (67 M weights in 16 tensors, bf16 copies: 295 us, 6.8 TB/s; 150 tensors of 5 to 1,000,003 elements, 17 M in all,
-// without: 72 us, 6.6 TB/s), HBM and the issue of instructions about equally with 8-bit ones (200 us, 6.1 TB/s; at 110 instructions an element it was 262
-// us, now there are 76; 24 to 36 bytes of a thread spilled for five blocks a multiprocessor).  Tensors are found by a binary search over their first tiles in the launch's parameters, so that one launch takes 320 of any
-// sizes. Whole blocks by 16-byte accesses (the tensors' addresses are on 16-byte boundaries), half a warp a block.  The last elements of a tensor go one by
-// one.
+// without: 73 us, 6.6 TB/s), HBM and the issue of instructions about equally with 8-bit ones (200 us, 6.1 TB/s; at 110 instructions an element it was 262
+// us, now there are 76; 24 to 36 bytes of a thread are spilled for five blocks a multiprocessor).  Tensors are found by a binary search over their first
+// tiles in the launch's parameters, so that one launch takes 320 of any sizes.  Whole blocks by 16-byte accesses (the tensors' addresses are on 16-byte
+// boundaries), half a warp a block.  The last elements of a tensor go one by one.
 template <typename TG, bool EIGHT, int N>
 __global__ void __launch_bounds__(kAdamThreads, EIGHT ? 5 : 1)
 adamw_kernel(const __grid_constant__ AdamParams<N> P) {

@@ -114,14 +114,13 @@ __device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
 //
 // What bounds it.  The tensor cores take 600 clocks for a k-block of a 256 x 256 tile, and 32 KB for it come into each SM.  Large products run at what
 // power and L2 allow: 2048 x 8192 x 8192 in 127 to 132 us from machine to machine (2080 to 2160 TFLOP/s; 1.07 GB from L2, 8.1 to 8.5 TB/s) in a burst,
-// 4096 x 8192 x 8192 in 235 to 245 us, 274 us (2010 TFLOP/s at 1.48
-// GHz and 1 kW) when it goes on for seconds -- the same loop with all k-blocks added up in tensor memory, without scales, takes 218 and 250.  Small ones
-// are bound by what surrounds the k-blocks, some 5 to 8 us: 256 x 8192 x 8192 26 us (adjoint 25), 777 x 3120 x 1312 14.6 us.  256 columns in runs spill 36
-// bytes a thread.  On the way (2048 x 8192 x 8192, us): an
-// arrival at the other block with release at the cluster's scope, a fence for every warp and k-block, 336; without 192; scalar sums instead of pairs put
-// together by moves 167; pairs that go on from tile to tile 152; one barrier for a product and its stage instead of two 143; eight summing warps with
-// 64-column loads instead of sixteen with 32-column ones 135; a second thread that issues products 127. Halves of tiles for the last turn cost the other
-// turns more than they gained (133).
+// 4096 x 8192 x 8192 in 235 to 245 us, 274 us (2010 TFLOP/s at 1.48 GHz and 1 kW) when it goes on for seconds -- the same loop with all k-blocks added
+// up in tensor memory, without scales, takes 218 and 250.  Small ones are bound by what surrounds the k-blocks, some 5 to 8 us: 256 x 8192 x 8192 26 us
+// (adjoint 25), 777 x 3120 x 1312 14.6 us.  256 columns in runs spill 36 bytes a thread.  On the way (2048 x 8192 x 8192, us): an arrival at the other
+// block with release at the cluster's scope, a fence for every warp and k-block, 336; without 192; scalar sums instead of pairs put together by moves
+// 167; pairs that go on from tile to tile 152; one barrier for a product and its stage instead of two 143; eight summing warps with 64-column loads
+// instead of sixteen with 32-column ones 135; a second thread that issues products 127. Halves of tiles for the last turn cost the other turns more than
+// they gained (133).
 // ------------------------------------------------------------------------------------------
 constexpr int kF8Tail = 1024 + 512;                         // alignment, barriers
 constexpr int kF8ScaleSlots = 8;                            // k-blocks whose scales are on their way or waited for
